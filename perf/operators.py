@@ -171,7 +171,7 @@ def prepare(case, seed):
             st["kp"], st["vp"] = (normal(n_phys, hkv, g, d).to(dt) for _ in range(2))
             st["ks"] = st["vs"] = None
         elif case["kv"] == "fp8":
-            st["kp"], st["vp"] = (normal(n_phys, hkv, g, d).mul_(100).to(torch.float8_e4m3fn).view(torch.uint8) for _ in range(2))
+            st["kp"], st["vp"] = (normal(n_phys, hkv, g, d).mul_(100).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for _ in range(2))
             st["ks"], st["vs"] = (torch.full((n_phys, hkv), 2.0 ** -6, device="cuda") for _ in range(2))
         else:
             (st["kp"], st["ks"]), (st["vp"], st["vs"]) = (_int4_encode(normal(n_phys, hkv, g, d)) for _ in range(2))
