@@ -382,9 +382,10 @@ def _exact_quantise(x):
 def _exact_fp8(page):
     """What an FP8 page [.., g, d] holds."""
     amax = page.abs().amax((-1, -2), keepdim=True)
-    scale = 2.0 ** torch.ceil(torch.log2(amax.clamp_min(1e-30) / 448.0)).clamp(-6, 7)
+    m, e = torch.frexp(amax / 448.0)                            # m 2^e, m from 0.5 up
+    scale = torch.exp2((e - (m == 0.5).int()).clamp(-6, 7).double())
     code = (page / scale).clamp(-448, 448)
-    step = 2.0 ** (torch.floor(torch.log2(code.abs().clamp_min(2.0 ** -6))) - 3)
+    step = torch.exp2((torch.frexp(code.abs().clamp_min(2.0 ** -6))[1] - 4).double())
     return torch.round(code / step) * step, scale
 
 
