@@ -71,6 +71,7 @@ extern "C" {
 
 #define LOSA_KV_NATIVE    0
 #define LOSA_KV_FP8_E4M3  1
+#define LOSA_KV_INT4      2
 
 #define LOSA_MAX_BLOCK 64
 
@@ -105,6 +106,9 @@ typedef struct {
                                /* the scales below; summaries stay `dtype` (bf16 contexts only)  */
   float*         k_scale;      /* [n_phys_pages, H_kv] power-of-two scale of each key page       */
   float*         v_scale;      /* [n_phys_pages, H_kv] likewise for the values; NULL when native */
+                               /* LOSA_KV_INT4: half a byte per element (strides in bytes; d/2   */
+                               /* contiguous bytes per token), and both scale arrays are byte    */
+                               /* arrays [n_phys_pages, H_kv, g, d/32]; see "4-bit pages" below  */
 } losa_kv_t;
 
 /* Per-block LoSA cache (Section 4.3 / "Memory overhead" in Section 4.5): B(d+1) scalars per head
@@ -341,10 +345,68 @@ int32_t losa_update_prefix_cache(losa_ctx* ctx, losa_kv_t* kv, losa_state_t* sta
  * (the summaries are those of the dequantised keys); block finalisation re-quantises every touched page from its dequantised old rows and the
  * new rows together.  Inputs must satisfy |x| <= 448 * 2^7 (larger magnitudes saturate).
  *
- * losa_quantize_kv_pages: src is a native bf16 cache, dst an FP8 cache with the same page_table,
+ * losa_quantize_kv_pages: src is a native bf16 cache, dst an FP8 (or 4-bit) cache with the same page_table,
  *   kv_len and n_phys_pages; writes dst's codes and scales for every logical page p < P_s of every
  *   sequence and dst's kmin / kmax. */
 int32_t losa_quantize_kv_pages(losa_ctx* ctx, const losa_kv_t* src, losa_kv_t* dst, void* stream);
+
+/* 4-bit pages (bf16 contexts) — an extension of the cache format like the FP8 one.  A cache with kv_format =
+ * LOSA_KV_INT4 keeps every K / V element as a 4-bit code and, for every run of 32 elements of a token's row, one
+ * scale byte:  amax = largest |x| of the run;  scale = the smallest number of four significant bits that is >=
+ * amax / 7, clamped to [2^-12, 960], and its byte b holds five exponent and three mantissa bits (b << 7 is the
+ * scale as an fp16 number);  code = x / scale rounded to the nearest integer, halves away from zero, clamped to
+ * +-7, and stored as code + 8, element 2j of the row in the low half of byte j, element 2j + 1 in the high half.
+ * The value every stage works with is scale * code: seven significant bits at most, exact in bf16 and fp16.
+ * A row takes d/2 + d/32 bytes, 68 instead of 256 at d = 128.  A token's codes depend on that token alone, so
+ * appending leaves the others as they are.  Slots past the prefix's end hold anything and are not read into a result.
+ * Stages 2, 3, 5 are unchanged (the summaries are those of the values the codes stand for); stage 4, the whole step,
+ * block finalisation, losa_quantize_kv_pages (dst), losa_build_page_summaries and the two calls below take such a
+ * cache.  The scale arrays must be 16-byte aligned.  Inputs must satisfy |x| <= 6720 (larger magnitudes saturate). */
+
+/* Rotation of queries and keys by position, a caller-owned table: row p of cos / sin belongs to position p.
+ * Pair j of a head's first rot_dim elements is (x_j, x_{j + rot_dim/2}), or (x_2j, x_{2j+1}) with `interleaved` != 0, and becomes
+ *   (x cos - y sin, y cos + x sin)  of its pair (x, y), in fp32 with every product and sum rounded, then rounded once to `dtype`. */
+typedef struct {
+  const float* cos_table;   /* [n_pos, rot_dim/2] fp32, 16-byte aligned                             */
+  const float* sin_table;   /* likewise                                                             */
+  int32_t n_pos;            /* positions in the table                                               */
+  int32_t rot_dim;          /* a multiple of 16, at most d; the rest of a head is left as it is     */
+  int32_t interleaved;      /* 0: pairs half the rotated part apart, else neighbours                */
+} losa_rope_t;
+
+/* New tokens of all sequences, one after the other: sequence s owns tokens cu[s] .. cu[s+1] - 1. */
+typedef struct {
+  const void *q, *k, *v;    /* [T] rows of H_q*d / H_kv*d / H_kv*d contiguous elements (dtype), 16-byte aligned */
+  int64_t q_stride, k_stride, v_stride;   /* elements from a token's row to the next; byte strides multiples of 16 */
+  const int32_t* cu;        /* [N+1] first token of each sequence; cu[N] = T; sequences may have none */
+  const int32_t* start;     /* [N] where each sequence's first new token goes; not the array kv->kv_len itself */
+  const int32_t* pos_opt;   /* [T] rotation position of every token, or NULL: its position in the sequence */
+  int32_t  n_tokens;        /* T                                                                    */
+  void*    q_out;           /* [T, H_q, d] rotated queries (may be q, if q is contiguous), or NULL: none wanted  */
+  void*    k_out;           /* [T, H_kv, d] keys as the cache now holds them (dequantised), or NULL  */
+  void*    v_out;           /* [T, H_kv, d] values likewise, or NULL                                 */
+} losa_new_tokens_t;
+
+/* Appending tokens to the paged cache, rotated on the way.  Token i of sequence s goes to prefix position start[s] + i
+ * through page_table (whose entries for the touched pages must already name physical pages of this sequence alone); its key is
+ * rotated and rounded to `dtype`, and key and value are stored in the cache's format.  kmin / kmax of every touched page are
+ * recomputed over its valid tokens (left out when both are NULL), FP8 pages that are touched are re-quantised as by block
+ * finalisation, and kv_len[s] = start[s] + its number of tokens (unchanged where that number is 0), so a sequence can also be
+ * taken back to an earlier length and continued from there.  A sequence whose tokens do not fit its page-table row or, without
+ * pos_opt, the rotation table, is left as it is (q_out, k_out, v_out too) and reported as LOSA_ERR_BOUNDS; with pos_opt a token
+ * whose position lies outside the table is taken unrotated and reported.
+ *   kv NULL: nothing is stored; q -> q_out and k -> k_out (both optional) are rotated only.  v, v_out and, with pos_opt, start are not used.
+ *   rope NULL: nothing is rotated (values as they are are appended). */
+int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, const losa_new_tokens_t* tokens, void* stream);
+
+/* Attention of all block tokens over the whole of a 4-bit cache (Section 2.2 for every token and every page): for every
+ * sequence s, token i and head h over t < kv_len[s]:  s_t = sm_scale * <q, k_t>;  L = log sum_t exp(s_t);
+ * out = sum_t exp(s_t - L) v_t.  With block_size 1 this is a decoding step's attention.  q, out [N, B, H_q, d] (bf16);
+ * lse_opt [N, B, H_q] fp32 or NULL.  kv_len[s] = 0 gives out = 0, L = -inf; a longer kv_len than the page-table row holds is
+ * cut to it and reported (LOSA_ERR_BOUNDS).  Keys, values and queries are fp16 operands that hold them exactly (a query element below
+ * 2^-28 of its row's largest loses low bits), softmax weights are rounded to fp16 (11 significant bits) before
+ * their product with the values; sums are fp32.  Another kv_format returns LOSA_ERR_UNSUPPORTED. */
+int32_t losa_int4_attn(losa_ctx* ctx, const void* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream);
 
 /* Set-up helper — per-page min/max keys of Section 2.3 for the whole prefix: kmin/kmax of every
  * logical page p < P_s over its valid tokens. */

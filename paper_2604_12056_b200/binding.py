@@ -31,6 +31,7 @@ EXPORTS = [
     "losa_profile_stage4", "losa_stage4_last_ms", "losa_select_active_static",
     "losa_denoise_step", "losa_select_active_tau", "losa_page_scores_topk_pooled",
     "losa_set_pooled_selection", "losa_set_step_selector", "losa_set_wait_limit", "losa_page_scores_topk_mma", "losa_quantize_kv_pages",
+    "losa_rope_append", "losa_int4_attn",
 ]
 
 
@@ -57,6 +58,17 @@ class KvT(C.Structure):
 class StateT(C.Structure):
     _fields_ = [("q_prev", C.c_void_p), ("o_p", C.c_void_p), ("lse_p", C.c_void_p), ("step", C.c_void_p),
                 ("o_p_format", C.c_int32)]
+
+
+class RopeT(C.Structure):
+    _fields_ = [("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
+class NewTokensT(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("cu", C.c_void_p), ("start", C.c_void_p), ("pos_opt", C.c_void_p),
+                ("n_tokens", C.c_int32), ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p)]
 
 
 class StepBuffersT(C.Structure):
@@ -89,6 +101,7 @@ _SIGNATURES = {
     "losa_page_scores_topk_pooled": "ppppppippp", "losa_page_scores_topk_mma": "ppppppippp",
     "losa_page_union": "ppppippppp", "losa_sparse_prefix_attn": "ppppppppp", "losa_block_attn_merge": "pppppppp",
     "losa_update_prefix_cache": "ppppppip", "losa_quantize_kv_pages": "pppp", "losa_build_page_summaries": "ppp",
+    "losa_rope_append": "ppppp", "losa_int4_attn": "pppppp",
     "losa_denoise_step": "ppppppppppip", "losa_denoise_step_host": "pppppppppip",
 }
 _typed = None
@@ -131,22 +144,52 @@ def torch_dtype(dtype: int):
     return torch.bfloat16 if dtype == LOSA_BF16 else torch.float32
 
 
-LOSA_KV_NATIVE, LOSA_KV_FP8_E4M3 = 0, 1
+LOSA_KV_NATIVE, LOSA_KV_FP8_E4M3, LOSA_KV_INT4 = 0, 1, 2
 
 
 def make_kv(k_pages, v_pages, kmin, kmax, page_table, kv_len, k_scale=None, v_scale=None) -> KvT:
     """losa_kv_t over a [n_phys, H_kv, g, d] pool (any strides with contiguous token rows).  With
-    k_scale / v_scale ([n_phys, H_kv] fp32) the pools are uint8 tensors of E4M3 codes."""
+    k_scale / v_scale ([n_phys, H_kv] fp32) the pools are uint8 tensors of E4M3 codes; with uint8 scales
+    ([n_phys, H_kv, g, d/32]) they are [n_phys, H_kv, g, d/2] uint8 tensors of two 4-bit codes each."""
     sp, sh_, st, sd = k_pages.stride()
     assert sd == 1 and v_pages.stride() == k_pages.stride()
     fp8 = k_scale is not None
     assert (k_pages.dtype == torch.uint8) == fp8
+    int4 = fp8 and k_scale.dtype == torch.uint8
+    if int4:
+        for t in (k_scale, v_scale):
+            assert t.dtype == torch.uint8 and t.is_contiguous() and t.shape == (*k_pages.shape[:3], k_pages.shape[3] // 16)
     kv = KvT(k_pages.data_ptr(), v_pages.data_ptr(), sp, sh_, st,
              0 if kmin is None else kmin.data_ptr(), 0 if kmax is None else kmax.data_ptr(),
              page_table.data_ptr(), kv_len.data_ptr(), k_pages.shape[0],
-             LOSA_KV_FP8_E4M3 if fp8 else LOSA_KV_NATIVE, k_scale.data_ptr() if fp8 else 0, v_scale.data_ptr() if fp8 else 0)
+             LOSA_KV_INT4 if int4 else LOSA_KV_FP8_E4M3 if fp8 else LOSA_KV_NATIVE, k_scale.data_ptr() if fp8 else 0, v_scale.data_ptr() if fp8 else 0)
     kv._keep = (k_pages, v_pages, kmin, kmax, page_table, kv_len, k_scale, v_scale)
     return kv
+
+
+def make_rope(cos, sin, interleaved=False) -> RopeT:
+    """losa_rope_t over [n_pos, rot_dim/2] fp32 tables."""
+    assert cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.dim() == 2
+    r = RopeT(_ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], 1 if interleaved else 0)
+    r._keep = (cos, sin)
+    return r
+
+
+def make_new_tokens(q, k, v, cu, start, pos=None, q_out=None, k_out=None, v_out=None) -> NewTokensT:
+    """losa_new_tokens_t over [T, H, d] tensors whose heads are contiguous within a token's row (the rows may lie
+    anywhere, as parts of a packed projection do); any of q, k, v may be None where the call does not need it."""
+    T, strides = 0, []
+    for t in (q, k, v):
+        if t is not None:
+            assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
+            T = t.shape[0]
+        strides.append(0 if t is None else t.stride(0) if T > 1 else t.shape[1] * t.shape[2])
+    assert all(t is None or t.shape[0] == T for t in (q, k, v, q_out, k_out, v_out)) and (pos is None or pos.numel() == T)
+    assert all(t is None or t.dtype == torch.int32 for t in (cu, start, pos))
+    ptr = [None if t is None else t.data_ptr() for t in (q, k, v)]
+    n = NewTokensT(*ptr, *strides, _ptr(cu), _ptr(start), _ptr(pos), T, _ptr(q_out), _ptr(k_out), _ptr(v_out))
+    n._keep = (q, k, v, cu, start, pos, q_out, k_out, v_out)
+    return n
 
 
 LOSA_STATE_F32, LOSA_STATE_BF16 = 0, 1
@@ -293,6 +336,17 @@ def losa_update_prefix_cache(ctx, kv, state, q, k_blk, v_blk, finalize_block):
 def losa_quantize_kv_pages(ctx, src_kv, dst_kv):
     """bf16 cache -> FP8 cache (codes, per-page scales, summaries of the dequantised keys)."""
     ctx._check("losa_quantize_kv_pages", _typed_lib().losa_quantize_kv_pages(ctx._h, C.byref(src_kv), C.byref(dst_kv), _stream()))
+
+
+def losa_rope_append(ctx, kv, rope, tokens):
+    """Appends (rotated) new tokens to the paged cache; kv None: rotates only; rope None: appends only."""
+    ctx._check("losa_rope_append", _typed_lib().losa_rope_append(
+        ctx._h, None if kv is None else C.byref(kv), None if rope is None else C.byref(rope), C.byref(tokens), _stream()))
+
+
+def losa_int4_attn(ctx, q, kv, out, lse_opt=None):
+    """Attention of all block tokens over the whole of a 4-bit cache."""
+    ctx._check("losa_int4_attn", _typed_lib().losa_int4_attn(ctx._h, _ptr(q), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
 
 
 def losa_build_page_summaries(ctx, kv):

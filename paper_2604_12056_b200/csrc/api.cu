@@ -42,6 +42,7 @@ int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   L->union_bits = off;
   off = align_up(off + sizeof(uint32_t) * static_cast<size_t>(sh->batch) * sh->n_kv_heads * ((sh->max_pages_per_seq + 31) / 32), 256);
   L->union_tickets = off; off = align_up(off + sizeof(uint32_t) * sh->batch * sh->n_kv_heads, 256);
+  L->int4_tickets = off; off = align_up(off + sizeof(uint32_t) * 4 * L->n_segments, 256);
   L->delta = off;    off = align_up(off + sizeof(double) * sh->batch * sh->block_size, 256);
   L->scores = off;
   off = align_up(off + 2 * sizeof(float) * static_cast<size_t>(sh->batch) * sh->block_size * sh->n_q_heads * L->score_stride, 256);
@@ -77,12 +78,13 @@ int32_t check_kv(const losa_ctx* c, const losa_kv_t* kv, bool need_summaries) {
   if (need_summaries && (!kv->kmin || !kv->kmax)) return LOSA_ERR_INVALID_ARG;
   if (kv->n_phys_pages < 1) return LOSA_ERR_INVALID_ARG;
   const losa_shape_t& sh = c->shape;
-  if (kv->kv_format != LOSA_KV_NATIVE && kv->kv_format != LOSA_KV_FP8_E4M3) return LOSA_ERR_INVALID_ARG;
-  const bool fp8 = kv->kv_format == LOSA_KV_FP8_E4M3;
-  if (fp8 && (!kv->k_scale || !kv->v_scale)) return LOSA_ERR_INVALID_ARG;
-  if (fp8 && sh.dtype != LOSA_BF16) return LOSA_ERR_UNSUPPORTED;
-  const int64_t es = fp8 ? 1 : (sh.dtype == LOSA_BF16 ? 2 : 4);
-  if (kv->stride_tok < sh.head_dim || kv->stride_head < 1 || kv->stride_page < 1) return LOSA_ERR_INVALID_ARG;
+  if (kv->kv_format != LOSA_KV_NATIVE && kv->kv_format != LOSA_KV_FP8_E4M3 && kv->kv_format != LOSA_KV_INT4) return LOSA_ERR_INVALID_ARG;
+  const bool int4 = kv->kv_format == LOSA_KV_INT4, codes = int4 || kv->kv_format == LOSA_KV_FP8_E4M3;
+  if (codes && (!kv->k_scale || !kv->v_scale)) return LOSA_ERR_INVALID_ARG;
+  if (codes && sh.dtype != LOSA_BF16) return LOSA_ERR_UNSUPPORTED;
+  if (int4 && (!aligned16(kv->k_scale) || !aligned16(kv->v_scale))) return LOSA_ERR_UNSUPPORTED;
+  const int64_t es = codes ? 1 : (sh.dtype == LOSA_BF16 ? 2 : 4);
+  if (kv->stride_tok < (int4 ? sh.head_dim / 2 : sh.head_dim) || kv->stride_head < 1 || kv->stride_page < 1) return LOSA_ERR_INVALID_ARG;
   if ((kv->stride_tok * es) % 16 || (kv->stride_head * es) % 16 || (kv->stride_page * es) % 16) return LOSA_ERR_UNSUPPORTED;
   if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages) || (kv->kmin && !aligned16(kv->kmin)) ||
       (kv->kmax && !aligned16(kv->kmax)))
@@ -261,6 +263,8 @@ int32_t losa_sparse_prefix_attn(losa_ctx* ctx, const void* q, const losa_kv_t* k
   if (rc == LOSA_OK) rc = check_state_format(ctx, state);
   if (rc != LOSA_OK) return rc;
   if (!aligned16(q) || !aligned16(state->o_p)) return LOSA_ERR_UNSUPPORTED;
+  if (kv->kv_format == LOSA_KV_INT4)
+    return launch_int4_prefix_attn(ctx, q, kv, active_idx, n_active, union_pages, union_count, state, as_stream(stream));
   return launch_sparse_prefix_attn(ctx, q, kv, active_idx, n_active, union_pages, union_count, state, as_stream(stream));
 }
 
@@ -292,9 +296,52 @@ int32_t losa_quantize_kv_pages(losa_ctx* ctx, const losa_kv_t* src, losa_kv_t* d
   int32_t rc = check_kv(ctx, src, false);
   if (rc == LOSA_OK) rc = check_kv(ctx, dst, true);
   if (rc != LOSA_OK) return rc;
-  if (src->kv_format != LOSA_KV_NATIVE || dst->kv_format != LOSA_KV_FP8_E4M3 || src->n_phys_pages != dst->n_phys_pages)
+  if (src->kv_format != LOSA_KV_NATIVE || dst->kv_format == LOSA_KV_NATIVE || src->n_phys_pages != dst->n_phys_pages)
     return LOSA_ERR_INVALID_ARG;
+  if (dst->kv_format == LOSA_KV_INT4) return launch_int4_quantize(ctx, src, dst, as_stream(stream));
   return launch_fp8_quantize(ctx, src, dst, as_stream(stream));
+}
+
+int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, const losa_new_tokens_t* tk, void* stream) {
+  if (!ctx || !tk || tk->n_tokens < 0) return LOSA_ERR_INVALID_ARG;
+  const losa_shape_t& sh = ctx->shape;
+  const int64_t es = sh.dtype == LOSA_BF16 ? 2 : 4;
+  const bool by_position = !kv && rope && tk->pos_opt;      // the sequences do not matter
+  if (!by_position && (!tk->cu || !tk->start)) return LOSA_ERR_INVALID_ARG;
+  if ((tk->q_out && !tk->q) || (tk->k_out && !tk->k)) return LOSA_ERR_INVALID_ARG;
+  if (kv) {
+    const int32_t rc = check_kv(ctx, kv, false);
+    if (rc != LOSA_OK) return rc;
+    if (!tk->k || !tk->v || !kv->kmin != !kv->kmax || tk->start == kv->kv_len) return LOSA_ERR_INVALID_ARG;
+  } else if (!tk->q_out && !tk->k_out) {
+    return LOSA_ERR_INVALID_ARG;
+  }
+  if (rope) {
+    if (!rope->cos_table || !rope->sin_table || rope->n_pos < 1 || rope->rot_dim < 1 || rope->rot_dim > sh.head_dim) return LOSA_ERR_INVALID_ARG;
+    if (rope->rot_dim % 16 || !aligned16(rope->cos_table) || !aligned16(rope->sin_table)) return LOSA_ERR_UNSUPPORTED;
+  }
+  auto rows = [&](const void* x, int64_t stride, int heads) -> int32_t {     // a tensor of one row per token
+    if (!x || tk->n_tokens == 0) return LOSA_OK;
+    if (stride < static_cast<int64_t>(heads) * sh.head_dim && tk->n_tokens > 1) return LOSA_ERR_INVALID_ARG;
+    return aligned16(x) && (tk->n_tokens == 1 || stride * es % 16 == 0) ? LOSA_OK : LOSA_ERR_UNSUPPORTED;
+  };
+  int32_t rc = tk->q_out ? rows(tk->q, tk->q_stride, sh.n_q_heads) : LOSA_OK;
+  if (rc == LOSA_OK && (kv || tk->k_out)) rc = rows(tk->k, tk->k_stride, sh.n_kv_heads);
+  if (rc == LOSA_OK && kv) rc = rows(tk->v, tk->v_stride, sh.n_kv_heads);
+  if (rc != LOSA_OK) return rc;
+  if (!aligned16(tk->q_out) || !aligned16(tk->k_out) || !aligned16(tk->v_out)) return LOSA_ERR_UNSUPPORTED;
+  if (tk->q_out && tk->q_out == tk->q && tk->n_tokens > 1 && tk->q_stride != static_cast<int64_t>(sh.n_q_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
+  if (tk->k_out && tk->k_out == tk->k && tk->n_tokens > 1 && tk->k_stride != static_cast<int64_t>(sh.n_kv_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
+  if (tk->n_tokens == 0) return LOSA_OK;
+  return launch_rope_append(ctx, kv, rope, tk, as_stream(stream));
+}
+
+int32_t losa_int4_attn(losa_ctx* ctx, const void* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream) {
+  if (!ctx || !q || !out) return LOSA_ERR_INVALID_ARG;
+  const int32_t rc = check_kv(ctx, kv, false);
+  if (rc != LOSA_OK) return rc;
+  if (kv->kv_format != LOSA_KV_INT4 || !aligned16(q) || !aligned16(out)) return LOSA_ERR_UNSUPPORTED;
+  return launch_int4_attn(ctx, q, kv, out, lse_opt, as_stream(stream));
 }
 
 int32_t losa_build_page_summaries(losa_ctx* ctx, losa_kv_t* kv, void* stream) {
@@ -321,6 +368,15 @@ int32_t losa_denoise_step(losa_ctx* ctx, const void* q, const void* k_blk, const
   cudaStream_t st = as_stream(stream);
   const losa_shape_t& sh = ctx->shape;
   int32_t* slot_map = reinterpret_cast<int32_t*>(ctx->ws + ctx->lay.slot_map);
+  if (kv->kv_format == LOSA_KV_INT4) {             // 4-bit pages: the six stages one after the other
+    rc = launch_select_active(ctx, q, state->q_prev, sh.n_q_heads * sh.head_dim, m_per_seq, state->step, buf->active_idx, buf->n_active, nullptr, st);
+    if (rc == LOSA_OK) rc = launch_page_scores_topk(ctx, q, kv, buf->active_idx, buf->n_active, state->step, k, buf->topk_pages, nullptr, st, ctx->pooled_selection);
+    if (rc == LOSA_OK) rc = launch_page_union(ctx, buf->topk_pages, buf->active_idx, buf->n_active, k, kv->kv_len, state->step, buf->union_pages, buf->union_count, st);
+    if (rc == LOSA_OK) rc = launch_int4_prefix_attn(ctx, q, kv, buf->active_idx, buf->n_active, buf->union_pages, buf->union_count, state, st);
+    if (rc == LOSA_OK) rc = launch_block_attn_merge(ctx, q, k_blk, v_blk, state, out, lse_out_opt, st);
+    if (rc == LOSA_OK) rc = launch_update_prefix_cache(ctx, kv, state, q, k_blk, v_blk, 0, st);
+    return rc;
+  }
   // The in-block attention needs nothing from stages 1-4.  Where the selection ends in the candidate
   // refinement, that kernel's grid carries it; elsewhere (fp32, long lists) it runs on a second stream.
   const BlockInputs blk = {q, k_blk, v_blk};

@@ -329,9 +329,9 @@ int32_t launch_update_t(losa_ctx* c, losa_kv_t* kv, losa_state_t* state, const v
         static_cast<const uint4*>(q), static_cast<uint4*>(state->q_prev), n_vec, state->step, sh.batch);
     return after_launch(c);
   }
-  if (kv->kv_format == LOSA_KV_FP8_E4M3) {
-    // FP8 pages: the touched pages are re-quantised from their dequantised old rows and the new rows
-    int32_t rc = launch_fp8_append(c, kv, k_blk, v_blk, st);
+  if (kv->kv_format != LOSA_KV_NATIVE) {
+    // FP8 pages: the touched pages are re-quantised from their dequantised old rows and the new rows; 4-bit pages: only the new rows
+    int32_t rc = kv->kv_format == LOSA_KV_INT4 ? launch_int4_append(c, kv, k_blk, v_blk, st) : launch_fp8_append(c, kv, k_blk, v_blk, st);
     if (rc != LOSA_OK) return rc;
     launch_k(finalize_counters_kernel, 1, std::max(32, sh.batch), 0, st, kv->kv_len, state->step, sh.batch, sh.block_size,
              sh.page_size, sh.max_pages_per_seq);
@@ -411,6 +411,7 @@ int32_t launch_update_prefix_cache(losa_ctx* c, losa_kv_t* kv, losa_state_t* sta
 
 int32_t launch_build_page_summaries(losa_ctx* c, losa_kv_t* kv, cudaStream_t st) {
   if (kv->kv_format == LOSA_KV_FP8_E4M3) return launch_fp8_summaries(c, kv, st);
+  if (kv->kv_format == LOSA_KV_INT4) return launch_int4_summaries(c, kv, st);
   if (c->shape.dtype == LOSA_BF16)
     return c->shape.head_dim == 128 ? launch_summaries_t<__nv_bfloat16, 128>(c, kv, st) : launch_summaries_t<__nv_bfloat16, 64>(c, kv, st);
   return c->shape.head_dim == 128 ? launch_summaries_t<float, 128>(c, kv, st) : launch_summaries_t<float, 64>(c, kv, st);

@@ -19,38 +19,11 @@
 // the summaries are the encoded column extremes of the source; -0 orders below +0 in both.
 // Quantising 90,000 tokens of 8 heads x 128 (565 MB in and out): 261 us with a thread per column
 // that walked the tokens three times, 116 us now.
-#include <cuda_fp8.h>
-
 #include "kernels.h"
+#include "page_formats.cuh"
 
 namespace losa {
 namespace {
-
-// eight codes -> values, eight values -> codes (round to nearest even, saturate at +-448)
-__device__ __forceinline__ void fp8_decode8(uint2 w, float (&v)[8]) {
-  const uint32_t x[2] = {w.x, w.y};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(x[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ uint2 fp8_encode8(const float (&v)[8], float inv_scale) {
-  uint32_t x[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] * inv_scale, v[2 * i + 1] * inv_scale), __NV_SATFINITE, __NV_E4M3);
-  return make_uint2(x[0] | (x[1] << 16), x[2] | (x[3] << 16));
-}
-__device__ __forceinline__ float pow2f(int e) { return __int_as_float((127 + e) << 23); }   // -126 <= e <= 127
-// e = the smallest integer in [-6, 7] with amax <= 448 * 2^e = 1.75 * 2^(e + 8)
-__device__ __forceinline__ int fp8_scale_exp(float amax) {
-  const uint32_t b = __float_as_uint(amax);
-  const int e = static_cast<int>(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return min(7, max(-6, e));
-}
 
 struct Fp8Params {
   const __nv_bfloat16* k_src;        // bf16 pool (quantise) — strides below; null otherwise

@@ -99,6 +99,17 @@ int32_t launch_fp8_quantize(losa_ctx* c, const losa_kv_t* src, losa_kv_t* dst, c
 int32_t launch_fp8_summaries(losa_ctx* c, losa_kv_t* kv, cudaStream_t st);
 int32_t launch_fp8_append(losa_ctx* c, losa_kv_t* kv, const void* k_blk, const void* v_blk, cudaStream_t st);
 
+// New tokens into the paged cache, rotated on the way (kv null: rotation only; rope null: no rotation).
+int32_t launch_rope_append(losa_ctx* c, losa_kv_t* kv, const losa_rope_t* rope, const losa_new_tokens_t* tk, cudaStream_t st);
+// 4-bit pages (bf16 contexts): a bf16 pool page by page, summaries of what is there, append of a block.
+int32_t launch_int4_quantize(losa_ctx* c, const losa_kv_t* src, losa_kv_t* dst, cudaStream_t st);
+int32_t launch_int4_summaries(losa_ctx* c, losa_kv_t* kv, cudaStream_t st);
+int32_t launch_int4_append(losa_ctx* c, losa_kv_t* kv, const void* k_blk, const void* v_blk, cudaStream_t st);
+// Attention over 4-bit pages: all block tokens over the whole cache, or (stage 4) the active tokens over the listed pages.
+int32_t launch_int4_attn(losa_ctx* c, const void* q, const losa_kv_t* kv, void* out, float* lse_opt, cudaStream_t st);
+int32_t launch_int4_prefix_attn(losa_ctx* c, const void* q, const losa_kv_t* kv, const int32_t* active_idx, const int32_t* n_active,
+                                const int32_t* union_pages, const int32_t* union_count, losa_state_t* state, cudaStream_t st);
+
 // Largest k and page count the top-k kernel's shared memory allows for this context.
 int32_t topk_max_sortable(const losa_ctx* c);
 
