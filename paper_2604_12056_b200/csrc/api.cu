@@ -308,20 +308,21 @@ int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, 
   const int64_t es = sh.dtype == LOSA_BF16 ? 2 : 4;
   const bool by_position = !kv && rope && tk->pos_opt;      // the sequences do not matter
   if (!by_position && (!tk->cu || !tk->start)) return LOSA_ERR_INVALID_ARG;
-  if ((tk->q_out && !tk->q) || (tk->k_out && !tk->k)) return LOSA_ERR_INVALID_ARG;
+  const bool none = tk->n_tokens == 0;                       // (no rows: their pointers may be null)
+  if (!none && ((tk->q_out && !tk->q) || (tk->k_out && !tk->k))) return LOSA_ERR_INVALID_ARG;
   if (kv) {
     const int32_t rc = check_kv(ctx, kv, false);
     if (rc != LOSA_OK) return rc;
-    if (!tk->k || !tk->v || !kv->kmin != !kv->kmax || tk->start == kv->kv_len) return LOSA_ERR_INVALID_ARG;
-  } else if (!tk->q_out && !tk->k_out) {
+    if ((!none && (!tk->k || !tk->v)) || !kv->kmin != !kv->kmax || tk->start == kv->kv_len) return LOSA_ERR_INVALID_ARG;
+  } else if (!none && !tk->q_out && !tk->k_out) {
     return LOSA_ERR_INVALID_ARG;
   }
   if (rope) {
     if (!rope->cos_table || !rope->sin_table || rope->n_pos < 1 || rope->rot_dim < 1 || rope->rot_dim > sh.head_dim) return LOSA_ERR_INVALID_ARG;
     if (rope->rot_dim % 16 || !aligned16(rope->cos_table) || !aligned16(rope->sin_table)) return LOSA_ERR_UNSUPPORTED;
   }
+  if (none) return LOSA_OK;
   auto rows = [&](const void* x, int64_t stride, int heads) -> int32_t {     // a tensor of one row per token
-    if (!x || tk->n_tokens == 0) return LOSA_OK;
     if (stride < static_cast<int64_t>(heads) * sh.head_dim && tk->n_tokens > 1) return LOSA_ERR_INVALID_ARG;
     return aligned16(x) && (tk->n_tokens == 1 || stride * es % 16 == 0) ? LOSA_OK : LOSA_ERR_UNSUPPORTED;
   };
@@ -332,7 +333,6 @@ int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, 
   if (!aligned16(tk->q_out) || !aligned16(tk->k_out) || !aligned16(tk->v_out)) return LOSA_ERR_UNSUPPORTED;
   if (tk->q_out && tk->q_out == tk->q && tk->n_tokens > 1 && tk->q_stride != static_cast<int64_t>(sh.n_q_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
   if (tk->k_out && tk->k_out == tk->k && tk->n_tokens > 1 && tk->k_stride != static_cast<int64_t>(sh.n_kv_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
-  if (tk->n_tokens == 0) return LOSA_OK;
   return launch_rope_append(ctx, kv, rope, tk, as_stream(stream));
 }
 

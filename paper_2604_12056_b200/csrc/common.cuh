@@ -243,6 +243,15 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
   }
 }
+// The same for waits that as a rule are over before they begin: a bound that is shorter than a look at the barrier takes has
+// run out by then, whatever the look would find (which is how the way out is exercised).
+constexpr long long kLookCycles = 32;
+__device__ __forceinline__ bool mbar_wait_or_expire(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, long long limit) {
+  if (limit >= kLookCycles) return mbar_wait(bar, parity, abort_flag, status, limit);
+  *abort_flag = 1;
+  set_status(status, LOSA_ERR_TIMEOUT);
+  return false;
+}
 // Wait of a CTA that has given up, for work it had already put in flight (page copies into its
 // shared memory, tensor-core instructions on its tensor memory): bounded by kDrainCycles, ignores
 // the abort flag, reports nothing (the status word already holds the reason).

@@ -287,7 +287,7 @@ int4_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     int k = 0;
     for (; k < mine; ++k) {
       const uint32_t use = stage_use + k, st = use % S;
-      ok = __all_sync(0xffffffffu, mbar_wait(bars0 + 8 * st, (use / S) & 1, abort_flag, p.status, p.wait_cycles));
+      ok = __all_sync(0xffffffffu, mbar_wait_or_expire(bars0 + 8 * st, (use / S) & 1, abort_flag, p.status, p.wait_cycles));
       if (!ok) break;
       const int valid = valid_s[st];
       const uint32_t ck = codes0 + st * UC, cv = ck + UC / 2, ks = scales0 + st * US, vs = ks + US / 2;

@@ -34,7 +34,7 @@ class LosaLayer:
 
     def __init__(self, cfg, k_pages, v_pages, page_table, kv_len, mode="losa", device="cuda",
                  share_pool_with: "LosaLayer | None" = None, tau: float = 0.0, pooled: bool = False,
-                 mma_selector: bool = False, fp8_kv: bool = False, state_bf16: bool = False):
+                 mma_selector: bool = False, fp8_kv: bool = False, state_bf16: bool = False, int4_kv: bool = False):
         self.cfg, self.mode, self.device = cfg, mode, device
         self.tau = tau            # > 0: stage 1 keeps tokens until their Delta reach tau of the block's total
         self.pooled = pooled      # stage 2 keeps one page list per (token, KV head) instead of one per query head
@@ -61,7 +61,16 @@ class LosaLayer:
             self.page_table = page_table if isinstance(page_table, torch.Tensor) else to_device(page_table, device)
         self.kv_len = (kv_len.clone() if isinstance(kv_len, torch.Tensor) else to_device(kv_len, device))
         self.kv = B.make_kv(self.k_pages, self.v_pages, self.kmin, self.kmax, self.page_table, self.kv_len)
-        self.fp8_kv = fp8_kv
+        self.fp8_kv, self.int4_kv = fp8_kv, int4_kv
+        if int4_kv:
+            # 4-bit cache with a scale byte per run of 32 elements of a row, quantised from the bf16 pools likewise
+            assert share_pool_with is None and not fp8_kv and self.dtype == B.LOSA_BF16
+            codes, scales = (*self.k_pages.shape[:3], d // 2), (*self.k_pages.shape[:3], d // 32)
+            self.k_codes, self.v_codes = (torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2))
+            self.k_scale, self.v_scale = (torch.zeros(scales, dtype=torch.uint8, device=device) for _ in range(2))
+            self.kv_native = self.kv
+            self.kv = B.make_kv(self.k_codes, self.v_codes, self.kmin, self.kmax, self.page_table, self.kv_len,
+                                self.k_scale, self.v_scale)
         if fp8_kv:
             # FP8 (E4M3) cache with one power-of-two scale per (page, KV head): quantised from the bf16
             # pools by the library, which also writes the summaries of the dequantised keys; every
@@ -92,7 +101,7 @@ class LosaLayer:
         self.union_count = torch.zeros((N, Hkv), dtype=torch.int32, device=device)
         self.out = torch.zeros((N, Bk, Hq, d), dtype=td, device=device)
         self.lse_out = torch.zeros((N, Bk, Hq), dtype=torch.float32, device=device)
-        if fp8_kv:
+        if fp8_kv or int4_kv:
             B.losa_quantize_kv_pages(self.ctx, self.kv_native, self.kv)
         elif share_pool_with is None:
             B.losa_build_page_summaries(self.ctx, self.kv)
@@ -133,6 +142,15 @@ class LosaLayer:
                                             self.union_count.data_ptr())
         B.losa_denoise_step(self.ctx, q, k_blk, v_blk, self.out, self.lse_out, self.kv, self.state,
                             self._step_buf, m_per_seq, self.cfg.topk)
+
+    def append(self, tokens, rope=None):
+        """New tokens of any number per sequence (binding.make_new_tokens) into the cache, rotated by `rope`
+        (binding.make_rope) where one is given."""
+        B.losa_rope_append(self.ctx, self.kv, rope, tokens)
+
+    def rotate(self, tokens, rope):
+        """The tokens' queries and keys rotated, with nothing appended (a denoising step's inputs)."""
+        B.losa_rope_append(self.ctx, None, rope, tokens)
 
     def finalize_block(self, k_blk, v_blk):
         B.losa_update_prefix_cache(self.ctx, self.kv, self.state, None, k_blk, v_blk, True)
