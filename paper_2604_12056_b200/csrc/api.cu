@@ -42,8 +42,8 @@ int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   L->union_bits = off;
   off = align_up(off + sizeof(uint32_t) * static_cast<size_t>(sh->batch) * sh->n_kv_heads * ((sh->max_pages_per_seq + 31) / 32), 256);
   L->union_tickets = off; off = align_up(off + sizeof(uint32_t) * sh->batch * sh->n_kv_heads, 256);
-  L->int4_tickets = off; off = align_up(off + sizeof(uint32_t) * 4 * L->n_segments, 256);
   L->delta = off;    off = align_up(off + sizeof(double) * sh->batch * sh->block_size, 256);
+  L->int4_records = off; off = align_up(off + 2 * sizeof(int32_t) * 16 * L->n_segments, 256);
   L->scores = off;
   off = align_up(off + 2 * sizeof(float) * static_cast<size_t>(sh->batch) * sh->block_size * sh->n_q_heads * L->score_stride, 256);
   L->partials = off;

@@ -24,7 +24,7 @@ struct WorkspaceLayout {
   size_t slot_map;   // int32[N*B] : slot of every block token in the active list of the whole-step path, -1 = stable
   size_t union_bits;    // uint32[N*H_kv*ceil(P_max/32)] : page bitmaps of the selection.  bf16: the selection writes the union from them, all zero between launches; fp32: stage 4 does, and stage 1 of the next whole step clears them
   size_t union_tickets; // uint32[N*H_kv] : its arrival counters (self-resetting)
-  size_t int4_tickets;  // uint32[4 * n_segments] : arrival counters of the 4-bit attention's segments (self-resetting)
+  size_t int4_records;  // int2[16 * n_segments] : likewise for the 4-bit attention, whose row groups are smaller
   size_t delta;      // double[N*B]
   size_t scores;     // float[2*N*B*H_q*score_stride]: page scores, or (lower, upper) bound pairs of them
   size_t partials;   // float[n_slots * kRowsPerGroup * (d + 2)]
@@ -36,16 +36,6 @@ struct WorkspaceLayout {
   int32_t n_ctas;        // CTAs of the split-KV attention kernels (one per SM)
   int32_t n_row_groups;  // ceil(B*G / kRowsPerGroup)
   int32_t n_segments;    // N * H_kv * n_row_groups
-};
-
-// Cached TMA descriptors of 4-bit pools, and what they were made for.
-struct Int4Maps {
-  alignas(64) unsigned char k[128];
-  alignas(64) unsigned char v[128];
-  const void* key_k;
-  const void* key_v;
-  int64_t strides[3];
-  int32_t n_phys;
 };
 
 }  // namespace losa
@@ -84,7 +74,6 @@ struct losa_ctx {
   int32_t approx_attr_set;
   int32_t refine_attr_set;
   int32_t int4_attr_set;     // and for the 4-bit attention kernels, a bit each
-  losa::Int4Maps int4_maps;
   // optional timing of the stage-4 main kernel
   int32_t profile;
   cudaEvent_t ev_begin, ev_end;
@@ -242,15 +231,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
       return false;
     }
   }
-}
-// The same for waits that as a rule are over before they begin: a bound that is shorter than a look at the barrier takes has
-// run out by then, whatever the look would find (which is how the way out is exercised).
-constexpr long long kLookCycles = 32;
-__device__ __forceinline__ bool mbar_wait_or_expire(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, long long limit) {
-  if (limit >= kLookCycles) return mbar_wait(bar, parity, abort_flag, status, limit);
-  *abort_flag = 1;
-  set_status(status, LOSA_ERR_TIMEOUT);
-  return false;
 }
 // Wait of a CTA that has given up, for work it had already put in flight (page copies into its
 // shared memory, tensor-core instructions on its tensor memory): bounded by kDrainCycles, ignores

@@ -3,10 +3,7 @@
 //
 // The pages to read form one flat list over (sequence, KV head, group of query rows), cut into equal shares, so
 // ragged batches leave no SM idle; partial results of a segment that several CTAs share meet by log-sum-exp.
-#include <cuda.h>
-
 #include <algorithm>
-#include <cstring>
 #include <type_traits>
 
 #include "kernels.h"
@@ -17,7 +14,8 @@ namespace {
 
 struct I4Params {
   const __nv_bfloat16* q;
-  const uint8_t *k_scale, *v_scale;
+  const uint8_t *k_pages, *v_pages, *k_scale, *v_scale;
+  int64_t stride_page, stride_head, stride_tok;
   const int32_t *page_table, *kv_len;
   const int32_t *active_idx, *n_active;            // null: all block tokens
   const int32_t *union_pages, *union_count;        // null: every page of the prefix
@@ -25,11 +23,10 @@ struct I4Params {
   float* lse;                                      // or null
   int out_bf16;
   float* partials;
-  uint32_t* tickets;
+  int2* seg_records;                                // per segment: first CTA and number of its records (0: none to merge)
   int32_t* status;
-  int N, B, Hq, Hkv, G, g, Pmax, n_phys, n_sk, n_rg, stages, min_units, bar_off;
+  int N, B, Hq, Hkv, G, g, Pmax, n_phys, n_sk, n_rg, min_units, pad;
   float sm_scale;
-  long long wait_cycles;
 };
 
 __device__ __forceinline__ int clamp_rows(int na, int B) { return na < 0 ? 0 : (na > B ? B : na); }
@@ -65,103 +62,42 @@ __device__ __forceinline__ float i4_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void i4_tma(uint32_t dst, const CUtensorMap* map, uint32_t bar, int t0, int kh, int phys, unsigned long long policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(t0), "r"(kh), "r"(phys), "l"(policy) : "memory");
-}
-__device__ __forceinline__ void i4_bulk(uint32_t dst, const uint8_t* src, uint32_t bar, uint32_t bytes) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
 #include "int4_attn_mma.cuh"
 
 // ===================================================================== host side
 constexpr int kI4SmemLimit = 232448;
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 int unit_tokens(const losa_shape_t& sh) { return std::min(32, sh.page_size); }
 
-int32_t encode_codes(losa_ctx* c, unsigned char* blob, const void* pool, const losa_kv_t* kv) {
-  const losa_shape_t& sh = c->shape;
-  if (!c->encode_fn) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    LOSA_CUDA_TRY(c, cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
-    if (!fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorSymbolNotFound);
-    c->encode_fn = fn;
-  }
-  const cuuint32_t row = static_cast<cuuint32_t>(sh.head_dim / 2);
-  const cuuint64_t dims[4] = {row, static_cast<cuuint64_t>(sh.page_size), static_cast<cuuint64_t>(sh.n_kv_heads), static_cast<cuuint64_t>(kv->n_phys_pages)};
-  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(kv->stride_tok), static_cast<cuuint64_t>(kv->stride_head), static_cast<cuuint64_t>(kv->stride_page)};
-  const cuuint32_t box[4] = {row, static_cast<cuuint32_t>(unit_tokens(sh)), 1, 1}, estr[4] = {1, 1, 1, 1};
-  const CUresult r = reinterpret_cast<EncodeTiledFn>(c->encode_fn)(
-      reinterpret_cast<CUtensorMap*>(blob), CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(pool), dims, strides, box, estr,
-      CU_TENSOR_MAP_INTERLEAVE_NONE, sh.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
-      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    c->last_cuda_error = static_cast<int32_t>(r);
-    return LOSA_ERR_CUDA;
-  }
-  return LOSA_OK;
-}
-
-int32_t ensure_code_maps(losa_ctx* c, const losa_kv_t* kv) {
-  losa::Int4Maps& m = c->int4_maps;
-  if (m.key_k == kv->k_pages && m.key_v == kv->v_pages && m.strides[0] == kv->stride_page && m.strides[1] == kv->stride_head &&
-      m.strides[2] == kv->stride_tok && m.n_phys == kv->n_phys_pages)
-    return LOSA_OK;
-  alignas(64) unsigned char k[128], v[128];
-  int32_t rc = encode_codes(c, k, kv->k_pages, kv);
-  if (rc == LOSA_OK) rc = encode_codes(c, v, kv->v_pages, kv);
-  if (rc != LOSA_OK) return rc;
-  memcpy(m.k, k, sizeof(k));
-  memcpy(m.v, v, sizeof(v));
-  m.key_k = kv->k_pages;
-  m.key_v = kv->v_pages;
-  m.strides[0] = kv->stride_page;
-  m.strides[1] = kv->stride_head;
-  m.strides[2] = kv->stride_tok;
-  m.n_phys = kv->n_phys_pages;
-  return LOSA_OK;
-}
-
-// where the barriers lie: behind the rings, whose place the merge tile takes
-template <int D, int NT>
-int mma_bar_off(int warps, int stages, int ut) {
-  return (std::max(warps * stages * (i4_unit_codes<D>(ut) + i4_unit_scales<D>(ut)), i4_merge_bytes<D, NT>(warps)) + 15) / 16 * 16;
-}
 template <int D, int NT>
 int mma_smem(int warps, int stages, int ut, int n_sk) {
-  return 1024 + mma_bar_off<D, NT>(warps, stages, ut) + warps * stages * (8 + 4) + 16 + kI4Head + (NT == 4 ? (D / 16) * NT * 32 * 8 : 0) + (n_sk + 1) * 4;
+  return 1024 + warps * (stages * (i4_unit_codes<D>(ut) + i4_unit_scales<D>(ut) + 4) + 8 * NT * D * 2) + i4_merge_bytes<D, NT>(warps) + (32 + n_sk + 1) * 4;
 }
 
 template <int D, int NT, int UT>
 int32_t launch_mma(losa_ctx* c, I4Params p, int max_rows, cudaStream_t st) {
   constexpr int R = 8 * NT;
-  auto kernel = int4_mma_kernel<D, NT, UT>;
-  const int bit = 1 << (NT == 1 ? 0 : NT == 2 ? 1 : 2);        // a context has one head dimension and one page size
+  constexpr int S = 2;
+  auto kernel = int4_mma_kernel<D, NT, UT, S>;
+  const int bit = NT;        // a context has one head dimension and one page size
   if (!(c->int4_attr_set & bit)) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kI4SmemLimit));
     c->int4_attr_set |= bit;
   }
   p.n_rg = (max_rows + R - 1) / R;
-  const int W = i4_warps(NT);
-  int stages = kI4Stages;
-  while (stages < 8 && mma_smem<D, NT>(W, stages + 1, UT, p.n_sk) <= kI4SmemLimit) ++stages;
-  p.stages = stages;
-  p.bar_off = mma_bar_off<D, NT>(W, stages, UT);
-  p.min_units = 2;
-  int grid = c->n_sms;
+  // Few segments: one CTA of all warps per SM.  More segments than SMs: CTAs of four warps, whose ends and starts overlap.
+  const bool many = p.n_sk * p.n_rg > c->n_sms;
+  const int W = many ? 4 : i4_warps(NT), per_sm = many ? i4_warps(NT) / 4 : 1;
+  p.min_units = 1;
+  p.pad = many ? 10 : 24;
+  int grid = c->n_sms * per_sm;
   grid = std::min<long long>(grid, static_cast<long long>(c->lay.n_slots) * kRowsPerGroup / (2 * R));      // room for the records
   if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
-  launch_k(kernel, grid, W * 32, mma_smem<D, NT>(W, stages, UT, p.n_sk), st, *reinterpret_cast<const CUtensorMap*>(c->int4_maps.k),
-           *reinterpret_cast<const CUtensorMap*>(c->int4_maps.v), p);
+  launch_k(kernel, grid, W * 32, mma_smem<D, NT>(W, S, UT, p.n_sk), st, p);
   if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
+  const int32_t rc = after_launch(c);
+  if (rc != LOSA_OK) return rc;
+  launch_k(int4_combine_kernel<D, R>, (p.n_sk * p.n_rg * R + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);
   return after_launch(c);
 }
 
@@ -169,21 +105,23 @@ template <int D, int UT>
 int32_t launch_rows(losa_ctx* c, const I4Params& p, cudaStream_t st) {
   const int max_rows = p.B * p.G;
   if (max_rows <= 8) return launch_mma<D, 1, UT>(c, p, max_rows, st);
-  if (max_rows <= 16) return launch_mma<D, 2, UT>(c, p, max_rows, st);
-  return launch_mma<D, 4, UT>(c, p, max_rows, st);
+  return launch_mma<D, 2, UT>(c, p, max_rows, st);
 }
 
 int32_t launch(losa_ctx* c, I4Params& p, const void* q, const losa_kv_t* kv, cudaStream_t st) {
   const losa_shape_t& sh = c->shape;
-  const int32_t rc = ensure_code_maps(c, kv);
-  if (rc != LOSA_OK) return rc;
   p.q = static_cast<const __nv_bfloat16*>(q);
+  p.k_pages = static_cast<const uint8_t*>(kv->k_pages);
+  p.v_pages = static_cast<const uint8_t*>(kv->v_pages);
+  p.stride_page = kv->stride_page;
+  p.stride_head = kv->stride_head;
+  p.stride_tok = kv->stride_tok;
   p.k_scale = reinterpret_cast<const uint8_t*>(kv->k_scale);
   p.v_scale = reinterpret_cast<const uint8_t*>(kv->v_scale);
   p.page_table = kv->page_table;
   p.kv_len = kv->kv_len;
   p.partials = reinterpret_cast<float*>(c->ws + c->lay.partials);
-  p.tickets = reinterpret_cast<uint32_t*>(c->ws + c->lay.int4_tickets);
+  p.seg_records = reinterpret_cast<int2*>(c->ws + c->lay.int4_records);
   p.status = status_ptr(c);
   p.N = sh.batch;
   p.B = sh.block_size;
@@ -195,7 +133,6 @@ int32_t launch(losa_ctx* c, I4Params& p, const void* q, const losa_kv_t* kv, cud
   p.n_phys = kv->n_phys_pages;
   p.n_sk = sh.batch * sh.n_kv_heads;
   p.sm_scale = sh.sm_scale;
-  p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
   const bool ut16 = unit_tokens(sh) == 16;
   if (sh.head_dim == 128) return ut16 ? launch_rows<128, 16>(c, p, st) : launch_rows<128, 32>(c, p, st);
   return ut16 ? launch_rows<64, 16>(c, p, st) : launch_rows<64, 32>(c, p, st);
