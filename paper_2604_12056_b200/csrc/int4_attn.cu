@@ -8,6 +8,7 @@
 
 #include "kernels.h"
 #include "page_formats.cuh"
+#include "tcgen05_ops.cuh"
 
 namespace losa {
 namespace {
@@ -26,7 +27,9 @@ struct I4Params {
   int2* seg_records;                                // per segment: first CTA and number of its records (0: none to merge)
   int32_t* status;
   int N, B, Hq, Hkv, G, g, Pmax, n_phys, n_sk, n_rg, min_units, pad;
+  int rows_above, rows_upto;                       // segments with as many query rows are this kernel's
   float sm_scale;
+  long long wait_cycles;                           // bound of every mbarrier wait, in SM clock cycles
 };
 
 __device__ __forceinline__ int clamp_rows(int na, int B) { return na < 0 ? 0 : (na > B ? B : na); }
@@ -57,17 +60,265 @@ __device__ __forceinline__ void i4_finish(const I4Params& p, int s, int kh, int 
   i4_store4(p, row * d + c, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (c == 0 && p.lse) p.lse[row] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
 }
-__device__ __forceinline__ float i4_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+// ===================================================================== codes into operands
+// A word of eight codes becomes four half2 operands with their scale in ten instructions: two shifts, and
+// for each half2 one LOP3 ((x & mask) | 0x6400: 1024 + 4u or 1024 + 64u as fp16) and one HFMA2 whose result,
+// scale * (u - 8) / 4, is exact: scales have four significant bits, so the addends 66 scale and 6 scale have ten and six.
+// (The quarter keeps 66 scale below fp16's end for scales up to 960; the softmax scale and the end result take it back.)
+//
+// (x & MASK) | 0x6400 of both halves, as one instruction
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t i4_take(uint32_t x) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(x), "n"(MASK), "r"(0x64006400u));
+  return d;
 }
+__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// multipliers and addends of the two places a code is taken from
+struct I4Scale { uint32_t m4, a4, m64, a64; };
+__device__ __forceinline__ I4Scale i4_scale(uint32_t s2) {     // s2: the scales of the two halves as fp16
+  I4Scale r;
+  r.m4 = mul_h2(s2, 0x2c002c00u);                    // 1 / 16
+  r.a4 = mul_h2(s2, 0xd420d420u);                    // -66
+  r.m64 = mul_h2(s2, 0x1c001c00u);                   // 1 / 256
+  r.a64 = mul_h2(s2, 0xc600c600u);                   // -6
+  return r;
+}
+// the four codes of each half of x -> h[0..3], each half2 one code of either half
+__device__ __forceinline__ void i4_operands(uint32_t x, const I4Scale& s, uint32_t (&h)[4]) {
+  const uint32_t y = x << 2, z = x >> 6;              // codes 0, 1 and 2, 3 of each half at bits 2 .. 5 and 6 .. 9
+  h[0] = fma_h2(i4_take<0x003c003cu>(y), s.m4, s.a4);
+  h[1] = fma_h2(i4_take<0x03c003c0u>(y), s.m64, s.a64);
+  h[2] = fma_h2(i4_take<0x003c003cu>(z), s.m4, s.a4);
+  h[3] = fma_h2(i4_take<0x03c003c0u>(z), s.m64, s.a64);
+}
+
+// ===================================================================== the list of work
+// A piece of a CTA's share: pages first_page .. of one (sequence, KV head, group of R query rows).
+struct I4Piece { int s, kh, rg, sk, seg_lo, pages, hi, first_page, n_units; };
+
+// The pages to read, over all segments (sequence, KV head, row group), as one list that is cut into equal shares.  Every segment
+// begins with `pad` positions that stand for no page: entering one costs a CTA about as much as that many pages.
+template <int D, int R>
+struct I4Work {
+  const I4Params& p;
+  int* pre;                                          // [n_sk + 1] charged positions before a (sequence, KV head)
+  int* runs;                                         // [32]
+  int upp_log, upp_mask, T, n_share, lo, hi, sk0;
+
+  // unit: tokens by which work is handed out inside a CTA (a page or a part of one)
+  __device__ __forceinline__ I4Work(const I4Params& params, int* prefix, int* run_sums, int unit) : p(params), pre(prefix), runs(run_sums) {
+    upp_log = p.g > unit ? (p.g == 2 * unit ? 1 : 2) : 0;
+    upp_mask = (1 << upp_log) - 1;
+  }
+  // query rows of a sequence that are this kernel's business
+  __device__ __forceinline__ int rows_of(int s) const {
+    const int rows = (p.n_active ? clamp_rows(p.n_active[s], p.B) : p.B) * p.G;
+    return rows > p.rows_above && rows <= p.rows_upto ? rows : 0;
+  }
+  __device__ __forceinline__ int pages_in(int sk) const {
+    if (p.union_count) return min(max(p.union_count[sk], 0), p.Pmax);
+    return min(max((p.kv_len[sk / p.Hkv] + p.g - 1) / p.g, 0), p.Pmax);
+  }
+  // All threads of the CTA: the prefix, this CTA's share; results of rows without any page; false: nothing (more) to do.
+  // least: units below which a share is not cut.
+  __device__ __forceinline__ bool begin(int least) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = blockDim.x >> 5;
+    const int n_runs = (p.n_sk + 31) >> 5;
+    for (int b = warp; b < n_runs; b += W) {         // runs of 32 by the warps, then the runs' sums
+      const int sk = b * 32 + lane;
+      int c = 0;
+      if (sk < p.n_sk) {
+        const int pages = pages_in(sk);
+        if (pages > 0) c = (pages + p.pad) * ((rows_of(sk / p.Hkv) + R - 1) / R);
+      }
+      int inc = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (sk < p.n_sk) pre[sk] = inc - c;
+      if (lane == 31) runs[b] = inc;
+    }
+    __syncthreads();
+    if (warp == 0) {
+      const int c = lane < n_runs ? runs[lane] : 0;
+      int inc = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      runs[lane] = inc - c;
+      if (lane == 31) pre[p.n_sk] = inc;
+    }
+    __syncthreads();
+    for (int i = 32 + tid; i < p.n_sk; i += blockDim.x) pre[i] += runs[i >> 5];
+    __syncthreads();
+    T = pre[p.n_sk];
+    n_share = max(1, min(static_cast<int>(gridDim.x), ((T << upp_log) + least - 1) / least));
+    for (int sk = blockIdx.x; sk < p.n_sk; sk += gridDim.x) {
+      const int s = sk / p.Hkv, kh = sk - s * p.Hkv, rows = rows_of(s), pages = pages_in(sk);
+      if (!p.union_count && kh == 0 && tid == 0 && (p.kv_len[s] + p.g - 1) / p.g > p.Pmax) set_status(p.status, LOSA_ERR_BOUNDS);
+      // no records to merge but those of the segments that have pages, which the CTAs that begin them write
+      for (int r = (pages > 0 ? (rows + R - 1) / R : 0) + tid; r < p.n_rg; r += blockDim.x) p.seg_records[sk * p.n_rg + r] = make_int2(0, 0);
+      if (pages > 0) continue;
+      for (int i = tid; i < rows * (D / 4); i += blockDim.x) {       // empty sums
+        const int r = i / (D / 4);
+        const long long row = i4_row(p, s, kh, r);
+        if (row >= 0) i4_store4(p, row * D + (i % (D / 4)) * 4, 0.f, 0.f, 0.f, 0.f);
+        if (row >= 0 && p.lse && i % (D / 4) == 0) p.lse[row] = -INFINITY;
+      }
+    }
+    if (static_cast<int>(blockIdx.x) >= n_share) return false;
+    lo = cta_lo(T, blockIdx.x, n_share);
+    hi = cta_lo(T, blockIdx.x + 1, n_share);
+    if (lo >= hi) return false;
+    int a = 0, b = p.n_sk;                           // pre[a] <= lo < pre[b]
+    while (b - a > 1) {
+      const int m = (a + b) >> 1;
+      if (pre[m] <= lo) a = m; else b = m;
+    }
+    sk0 = a;
+    return true;
+  }
+  // the piece at position item, whose (sequence, KV head) is `from` or one after it
+  __device__ __forceinline__ I4Piece piece_at(int item, int from) const {
+    I4Piece x;
+    x.sk = from;
+    while (pre[x.sk + 1] <= item) ++x.sk;
+    x.s = x.sk / p.Hkv;
+    x.kh = x.sk - x.s * p.Hkv;
+    const int groups = p.n_rg == 1 ? 1 : (rows_of(x.s) + R - 1) / R, all = pre[x.sk + 1] - pre[x.sk], length = groups == 1 ? all : all / groups;
+    x.rg = groups == 1 ? 0 : (item - pre[x.sk]) / length;
+    x.seg_lo = pre[x.sk] + x.rg * length;
+    x.pages = length - p.pad;
+    x.hi = min(hi, x.seg_lo + length);
+    x.first_page = max(0, item - x.seg_lo - p.pad);
+    x.n_units = (max(0, x.hi - x.seg_lo - p.pad) - x.first_page) << upp_log;
+    return x;
+  }
+  // the next one that has pages, or an empty one at the end
+  __device__ __forceinline__ I4Piece next_piece(int item, int from) const {
+    I4Piece x{};
+    x.hi = hi;
+    while (item < hi) {
+      x = piece_at(item, from);
+      if (x.n_units > 0) break;
+      item = x.hi;
+      from = x.sk;
+    }
+    return x;
+  }
+  // first CTA and number of the records of a segment that several CTAs share
+  __device__ __forceinline__ int2 records(const I4Piece& x) const {
+    return segment_records(T, n_share, x.seg_lo + p.pad, x.seg_lo + p.pad + x.pages);
+  }
+};
+
+// Physical page of entry `page` of a piece's list and its valid tokens from token t0 on, at most `most` of them (0: none).
+__device__ __forceinline__ int2 i4_resolve(const I4Params& p, const I4Piece& x, int entry, int t0, int most) {
+  const int page = p.union_pages ? p.union_pages[static_cast<size_t>(x.sk) * p.Pmax + entry] : entry;
+  int at = -1, left = 0;
+  if (page >= 0 && page < p.Pmax) {
+    at = p.page_table[static_cast<size_t>(x.s) * p.Pmax + page];
+    left = p.kv_len[x.s] - page * p.g;
+  }
+  if (at < 0 || at >= p.n_phys || left <= 0) {
+    set_status(p.status, LOSA_ERR_BOUNDS);
+    return make_int2(0, 0);
+  }
+  return make_int2(at, min(most, max(0, left - t0)));
+}
+
+// Segments that several CTAs share: a warp per row merges their records by log-sum-exp, in CTA order.
+constexpr int kI4CombineWarps = 4;
+template <int D, int R, bool BY_SEGMENT>
+__global__ void __launch_bounds__(kI4CombineWarps * 32) int4_combine_kernel(const __grid_constant__ I4Params p) {
+  grid_dep_wait();
+  const int lane = threadIdx.x & 31, w = blockIdx.x * kI4CombineWarps + (threadIdx.x >> 5);
+  const int seg = w / R, r = w % R;
+  if (seg >= p.n_sk * p.n_rg) return;
+  const int2 rec = p.seg_records[seg];
+  if (rec.y == 0) return;
+  const int sk = seg / p.n_rg, rg = seg - sk * p.n_rg, s = sk / p.Hkv, kh = sk - s * p.Hkv;
+  if (rg * R + r >= (p.n_active ? clamp_rows(p.n_active[s], p.B) : p.B) * p.G) return;
+  constexpr size_t kRecord = static_cast<size_t>(R) * (D + 2);
+  constexpr int C = D / 32, kBatch = 8;
+  // records of the CTAs one after the other, at CTA + segment; or two places per CTA, the first CTA's record in its second one, the
+  // others' in their first
+  const float* first = p.partials + (BY_SEGMENT ? static_cast<size_t>(rec.x + seg) : static_cast<size_t>(rec.x) * 2) * kRecord;
+  float acc[C], M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) acc[c] = 0.f;
+  for (int b = 0; b < rec.y; b += kBatch) {
+    float m[kBatch], l[kBatch], x[kBatch][C];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = b + i;
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[i][c] = 0.f;
+      if (j < rec.y) {
+        const float* at = first + (BY_SEGMENT ? j : 2 * j + (j == 0 ? 1 : 0)) * kRecord;
+        m[i] = at[r];
+        l[i] = at[R + r];
+        if constexpr (C == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(at + 2 * R + r * D + lane * 4);
+          x[i][0] = t.x; x[i][1] = t.y; x[i][2] = t.z; x[i][3] = t.w;
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(at + 2 * R + r * D + lane * 2);
+          x[i][0] = t.x; x[i][1] = t.y;
+        }
+      }
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, m[i]);
+    if (top == -INFINITY) continue;
+    const float keep = exp2f(M - top);
+    L *= keep;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] *= keep;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float f = exp2f(m[i] - top);
+      L = fmaf(l[i], f, L);
+#pragma unroll
+      for (int c = 0; c < C; ++c) acc[c] = fmaf(x[i][c], f, acc[c]);
+    }
+    M = top;
+  }
+  const long long row = i4_row(p, s, kh, rg * R + r);
+  if (row < 0) return;
+  const bool empty = L == 0.f;
+  const float inv = empty ? 0.f : 4.f / L;
+  if constexpr (C == 4) {
+    i4_store4(p, row * D + lane * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  } else {
+    // two columns a lane: pairs of lanes store four
+    const float o0 = __shfl_down_sync(0xffffffffu, acc[0], 1), o1 = __shfl_down_sync(0xffffffffu, acc[1], 1);
+    if ((lane & 1) == 0) i4_store4(p, row * D + lane * 2, acc[0] * inv, acc[1] * inv, o0 * inv, o1 * inv);
+  }
+  if (lane == 0 && p.lse) p.lse[row] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
 #include "int4_attn_mma.cuh"
+#include "int4_attn_tc.cuh"
 
 // ===================================================================== host side
 constexpr int kI4SmemLimit = 232448;
-
-int unit_tokens(const losa_shape_t& sh) { return std::min(32, sh.page_size); }
 
 template <int D, int NT>
 int mma_smem(int warps, int stages, int ut, int n_sk) {
@@ -97,15 +348,47 @@ int32_t launch_mma(losa_ctx* c, I4Params p, int max_rows, cudaStream_t st) {
   if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
   const int32_t rc = after_launch(c);
   if (rc != LOSA_OK) return rc;
-  launch_k(int4_combine_kernel<D, R>, (p.n_sk * p.n_rg * R + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);
+  launch_k(int4_combine_kernel<D, R, false>, (p.n_sk * p.n_rg * R + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);
   return after_launch(c);
 }
 
-template <int D, int UT>
-int32_t launch_rows(losa_ctx* c, const I4Params& p, cudaStream_t st) {
-  const int max_rows = p.B * p.G;
-  if (max_rows <= 8) return launch_mma<D, 1, UT>(c, p, max_rows, st);
-  return launch_mma<D, 2, UT>(c, p, max_rows, st);
+template <int D, int GP>
+int32_t launch_tc(losa_ctx* c, I4Params p, cudaStream_t st) {
+  auto kernel = int4_tc_kernel<D, GP>;
+  if (!(c->int4_attr_set & 4)) {
+    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kI4SmemLimit));
+    c->int4_attr_set |= 4;
+  }
+  static_assert(tc_smem<D>(kMaxSegments) <= kI4SmemLimit, "shared memory");
+  p.n_rg = c->lay.n_row_groups;
+  p.pad = 4 * (kTcTok / GP);                         // four groups' time
+  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
+  launch_k(kernel, c->lay.n_ctas, kTcWarps * 32, tc_smem<D>(p.n_sk), st, p);
+  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
+  const int32_t rc = after_launch(c);
+  if (rc != LOSA_OK) return rc;
+  launch_k(int4_combine_kernel<D, kTcRows, true>, (p.n_sk * p.n_rg * kTcRows + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);
+  return after_launch(c);
+}
+
+// The kernel with the rows on the tensor cores' M side takes 1.x times the other one's for 16 rows (per pass of 16), and one pass does for 128.
+constexpr int kI4MmaRows = 16;
+template <int D, int GP>
+int32_t launch_rows(losa_ctx* c, I4Params p, cudaStream_t st) {
+  constexpr int UT = GP < 32 ? GP : 32;
+  const int most = p.B * p.G;
+  p.rows_above = 0;
+  p.rows_upto = most;
+  if (most <= 8) return launch_mma<D, 1, UT>(c, p, most, st);
+  if (most <= kI4MmaRows) return launch_mma<D, 2, UT>(c, p, most, st);
+  if (p.n_active) {                                  // how many rows there are is known on the device only: each kernel takes its segments
+    p.rows_upto = kI4MmaRows;
+    const int32_t rc = launch_mma<D, 2, UT>(c, p, kI4MmaRows, st);
+    if (rc != LOSA_OK) return rc;
+    p.rows_above = kI4MmaRows;
+    p.rows_upto = most;
+  }
+  return launch_tc<D, GP>(c, p, st);
 }
 
 int32_t launch(losa_ctx* c, I4Params& p, const void* q, const losa_kv_t* kv, cudaStream_t st) {
@@ -133,9 +416,12 @@ int32_t launch(losa_ctx* c, I4Params& p, const void* q, const losa_kv_t* kv, cud
   p.n_phys = kv->n_phys_pages;
   p.n_sk = sh.batch * sh.n_kv_heads;
   p.sm_scale = sh.sm_scale;
-  const bool ut16 = unit_tokens(sh) == 16;
-  if (sh.head_dim == 128) return ut16 ? launch_rows<128, 16>(c, p, st) : launch_rows<128, 32>(c, p, st);
-  return ut16 ? launch_rows<64, 16>(c, p, st) : launch_rows<64, 32>(c, p, st);
+  p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
+  auto with_page = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    return sh.page_size == 16 ? launch_rows<D, 16>(c, p, st) : sh.page_size == 32 ? launch_rows<D, 32>(c, p, st) : launch_rows<D, 64>(c, p, st);
+  };
+  return sh.head_dim == 128 ? with_page(std::integral_constant<int, 128>{}) : with_page(std::integral_constant<int, 64>{});
 }
 
 }  // namespace

@@ -8,11 +8,6 @@
 //                                instruction thinks they are does not matter, Q's fragments are laid out the same way
 //   O^T[16 d x 8 rows]      += V^T[16 d x 16 tokens] P^T      A = values: a half2 is one element of two tokens, which two
 //                                byte permutes put together from the words of the two rows; P^T is S^T, transposed 8 x 8 by movmatrix
-// A word of eight codes becomes four half2 operands with their scale in ten instructions: two shifts, and
-// for each half2 one LOP3 ((x & mask) | 0x6400: 1024 + 4u or 1024 + 64u as fp16) and one HFMA2 whose result,
-// scale * (u - 8) / 4, is exact: scales have four significant bits, so the addends 66 scale and 6 scale have ten and six.
-// (The quarter keeps 66 scale below fp16's end for scales up to 960; the softmax scale and the end result take it back.)
-//
 // Warps take units of up to 32 tokens in turn, each through a ring of its own that it fills by asynchronous copies, 16 bytes per lane: no
 // barrier, and no instruction that one lane executes for the others (tensor copies, issued by one lane of each warp or by a warp
 // for all rings, cost 90 instructions a unit or kept the rings in step).  The rings run on over the pieces of a
@@ -31,41 +26,6 @@ template <int D> constexpr int i4_unit_scales(int ut) { return ut * D / 16; }   
 template <int D, int NT> constexpr int i4_merge_bytes(int warps) { return ((warps * 8 * NT * (D + 4) * 4 + warps * 8 * NT * 8) + 15) / 16 * 16; }
 constexpr int kI4Stride = 4;                        // floats between the rows of the merge tile: a row is D + 4
 
-// (x & MASK) | 0x6400 of both halves, as one instruction
-template <uint32_t MASK>
-__device__ __forceinline__ uint32_t i4_take(uint32_t x) {
-  uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(x), "n"(MASK), "r"(0x64006400u));
-  return d;
-}
-__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-// multipliers and addends of the two places a code is taken from
-struct I4Scale { uint32_t m4, a4, m64, a64; };
-__device__ __forceinline__ I4Scale i4_scale(uint32_t s2) {     // s2: the scales of the two halves as fp16
-  I4Scale r;
-  r.m4 = mul_h2(s2, 0x2c002c00u);                    // 1 / 16
-  r.a4 = mul_h2(s2, 0xd420d420u);                    // -66
-  r.m64 = mul_h2(s2, 0x1c001c00u);                   // 1 / 256
-  r.a64 = mul_h2(s2, 0xc600c600u);                   // -6
-  return r;
-}
-// the four codes of each half of x -> h[0..3], each half2 one code of either half
-__device__ __forceinline__ void i4_operands(uint32_t x, const I4Scale& s, uint32_t (&h)[4]) {
-  const uint32_t y = x << 2, z = x >> 6;              // codes 0, 1 and 2, 3 of each half at bits 2 .. 5 and 6 .. 9
-  h[0] = fma_h2(i4_take<0x003c003cu>(y), s.m4, s.a4);
-  h[1] = fma_h2(i4_take<0x03c003c0u>(y), s.m64, s.a64);
-  h[2] = fma_h2(i4_take<0x003c003cu>(z), s.m4, s.a4);
-  h[3] = fma_h2(i4_take<0x03c003c0u>(z), s.m64, s.a64);
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -122,107 +82,9 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
 
   grid_dep_trigger();                                // (the merging kernel comes up beside this one)
   grid_dep_wait();
-  auto rows_of = [&](int s) { return (p.n_active ? clamp_rows(p.n_active[s], p.B) : p.B) * p.G; };
-  auto pages_in = [&](int sk) {                      // pages of a segment
-    const int s = sk / p.Hkv;
-    if (p.union_count) return min(max(p.union_count[sk], 0), p.Pmax);
-    return min(max((p.kv_len[s] + p.g - 1) / p.g, 0), p.Pmax);
-  };
-  // prefix of the segments' lengths, `pad` pages added to each: runs of 32 by the warps, then the runs' sums
-  const int n_runs = (p.n_sk + 31) >> 5;
-  for (int b = warp; b < n_runs; b += W) {
-    const int sk = b * 32 + lane;
-    int c = 0;
-    if (sk < p.n_sk) {
-      const int pages = pages_in(sk);
-      if (pages > 0) c = (pages + p.pad) * ((rows_of(sk / p.Hkv) + R - 1) / R);
-    }
-    int inc = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += t;
-    }
-    if (sk < p.n_sk) pre[sk] = inc - c;
-    if (lane == 31) chunk_s[b] = inc;
-  }
-  __syncthreads();
-  if (warp == 0) {
-    const int c = lane < n_runs ? chunk_s[lane] : 0;
-    int inc = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += t;
-    }
-    chunk_s[lane] = inc - c;
-    if (lane == 31) pre[p.n_sk] = inc;
-  }
-  __syncthreads();
-  for (int i = 32 + tid; i < p.n_sk; i += blockDim.x) pre[i] += chunk_s[i >> 5];
-  __syncthreads();
-  const int T = pre[p.n_sk], upp = p.g / UT, upp_log = upp == 2 ? 1 : 0;    // units per page: one or two
-  // no more shares than give every warp min_units units
-  const int n_share = max(1, min(static_cast<int>(gridDim.x), (T * upp + W * p.min_units - 1) / (W * p.min_units)));
-  // rows without any page: empty sums
-  for (int sk = blockIdx.x; sk < p.n_sk; sk += gridDim.x) {
-    const int s = sk / p.Hkv, kh = sk - s * p.Hkv;
-    if (!p.union_count && kh == 0 && tid == 0 && (p.kv_len[s] + p.g - 1) / p.g > p.Pmax) set_status(p.status, LOSA_ERR_BOUNDS);
-    const int rows = rows_of(s);
-    if (pages_in(sk) > 0 && rows > 0) {
-      for (int r = (rows + R - 1) / R + tid; r < p.n_rg; r += blockDim.x) p.seg_records[sk * p.n_rg + r] = make_int2(0, 0);
-      continue;
-    }
-    for (int r = tid; r < p.n_rg; r += blockDim.x) p.seg_records[sk * p.n_rg + r] = make_int2(0, 0);
-    for (int i = tid; i < rows * (D / 4); i += blockDim.x) {
-      const int r = i / (D / 4);
-      const long long row = i4_row(p, s, kh, r);
-      if (row >= 0) i4_store4(p, row * D + (i % (D / 4)) * 4, 0.f, 0.f, 0.f, 0.f);
-      if (row >= 0 && p.lse && i % (D / 4) == 0) p.lse[row] = -INFINITY;
-    }
-  }
-  if (static_cast<int>(blockIdx.x) >= n_share) return;
-  const int lo = cta_lo(T, blockIdx.x, n_share), hi = cta_lo(T, blockIdx.x + 1, n_share);
-  if (lo >= hi) return;
-  int sk0 = 0;
-  {
-    int a = 0, b = p.n_sk;                           // pre[a] <= lo < pre[b]
-    while (b - a > 1) {
-      const int m = (a + b) >> 1;
-      if (pre[m] <= lo) a = m; else b = m;
-    }
-    sk0 = a;
-  }
-  // the pieces of the share: runs of pages of one (sequence, KV head, row group).  Every such segment begins with `pad` positions
-  // that stand for no page: entering one costs a CTA about as much as that many pages
-  struct Piece { int s, kh, rg, sk, seg_lo, pages, hi, first_page, n_units; };
-  auto piece_at = [&](int item, int from) {          // the piece at position item, whose segment is `from` or one after it
-    Piece x;
-    x.sk = from;
-    while (pre[x.sk + 1] <= item) ++x.sk;
-    x.s = x.sk / p.Hkv;
-    x.kh = x.sk - x.s * p.Hkv;
-    const int groups = p.n_rg == 1 ? 1 : (rows_of(x.s) + R - 1) / R, all = pre[x.sk + 1] - pre[x.sk], length = groups == 1 ? all : all / groups;
-    x.rg = groups == 1 ? 0 : (item - pre[x.sk]) / length;
-    x.seg_lo = pre[x.sk] + x.rg * length;
-    x.pages = length - p.pad;
-    x.hi = min(hi, x.seg_lo + length);
-    x.first_page = max(0, item - x.seg_lo - p.pad);
-    x.n_units = (max(0, x.hi - x.seg_lo - p.pad) - x.first_page) << upp_log;
-    return x;
-  };
-  auto next_piece = [&](int item, int from) {        // the next one that has pages, or an empty one at the end
-    Piece x{};
-    x.hi = hi;
-    while (item < hi) {
-      x = piece_at(item, from);
-      if (x.n_units > 0) break;
-      item = x.hi;
-      from = x.sk;
-    }
-    return x;
-  };
-
+  // no more shares than give every warp a unit
+  I4Work<D, R> work(p, pre, chunk_s, UT);
+  if (!work.begin(W * p.min_units)) return;
   // ---- the ring: units warp, warp + W, ... of every piece, one piece after the other; the copies run S - 1 units ahead
   unsigned long long policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -230,11 +92,11 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
   auto swz = [](int t, int chunk) { return D == 128 ? (chunk ^ ((t >> 1) & 3)) << 4 : chunk << 4; };   // (the same eight rows further on)
   const int64_t copy_src = static_cast<int64_t>(lane / LPR) * p.stride_tok + (lane % LPR) * 16;
   const uint32_t copy_dst = codes0 + (lane / LPR) * RB + swz(lane / LPR, lane % LPR), scale_dst = scales0 + lane * 4;
-  Piece ahead = next_piece(lo, sk0), piece = ahead;
+  I4Piece ahead = work.next_piece(work.lo, work.sk0), piece = ahead;
   int ahead_k = 0;                                   // the next unit to be copied: number ahead_k of this warp in its piece
   // queries of a piece, as they lie, into this warp's tile: with the next unit's copies
-  auto copy_queries = [&](const Piece& x) {
-    const int rows = rows_of(x.s) - x.rg * R;
+  auto copy_queries = [&](const I4Piece& x) {
+    const int rows = work.rows_of(x.s) - x.rg * R;
 #pragma unroll
     for (int i = 0; i < R * (D / 8) / 32; ++i) {
       const int r = (i * 32 + lane) / (D / 8), c = (i * 32 + lane) % (D / 8);
@@ -247,33 +109,19 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
   if (piece.n_units > 0) copy_queries(piece);
   int b_phys = 0, b_valid = 0;                       // physical pages and valid tokens of 32 of them, one per lane
   auto issue = [&](int ahead_slot) {                 // into this slot
-    while (warp + W * ahead_k >= ahead.n_units && ahead.hi < hi) {
-      ahead = next_piece(ahead.hi, ahead.sk);
+    while (warp + W * ahead_k >= ahead.n_units && ahead.hi < work.hi) {
+      ahead = work.next_piece(ahead.hi, ahead.sk);
       ahead_k = 0;
     }
     if (warp + W * ahead_k < ahead.n_units) {
       if ((ahead_k & 31) == 0) {
         const int u = warp + W * (ahead_k + lane);
-        b_phys = 0;
-        b_valid = 0;
-        if (u < ahead.n_units) {
-          const int pg = ahead.first_page + (u >> upp_log);
-          const int page = p.union_pages ? p.union_pages[static_cast<size_t>(ahead.sk) * p.Pmax + pg] : pg;
-          int at = -1, left = 0;
-          if (page >= 0 && page < p.Pmax) {
-            at = p.page_table[static_cast<size_t>(ahead.s) * p.Pmax + page];
-            left = p.kv_len[ahead.s] - page * p.g;
-          }
-          if (at < 0 || at >= p.n_phys || left <= 0) {
-            set_status(p.status, LOSA_ERR_BOUNDS);
-          } else {
-            b_phys = at;
-            b_valid = min(UT, max(0, left - (u & (upp - 1)) * UT));
-          }
-        }
+        const int2 at = u < ahead.n_units ? i4_resolve(p, ahead, ahead.first_page + (u >> work.upp_log), (u & work.upp_mask) * UT, UT) : make_int2(0, 0);
+        b_phys = at.x;
+        b_valid = at.y;
       }
       const int phys = __shfl_sync(0xffffffffu, b_phys, ahead_k & 31), valid = __shfl_sync(0xffffffffu, b_valid, ahead_k & 31);
-      const int t0 = ((warp + W * ahead_k) & (upp - 1)) * UT;
+      const int t0 = ((warp + W * ahead_k) & work.upp_mask) * UT;
       if (lane == 0) valid_s[ahead_slot] = valid;
       const int64_t src = phys * p.stride_page + ahead.kh * p.stride_head + t0 * p.stride_tok + copy_src;
       const uint8_t *ksrc = p.k_pages + src, *vsrc = p.v_pages + src;
@@ -316,7 +164,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
   const uint32_t at_vs0 = scales0 + US / 2 + row_v0 * RUNS + (D == 128 ? gid >> 1 : gid >> 2), at_vs1 = scales0 + US / 2 + row_v1 * RUNS + (D == 128 ? gid >> 1 : gid >> 2);
 
   while (piece.n_units > 0) {
-    const int s = piece.s, kh = piece.kh, rg = piece.rg, rows = rows_of(s), n_units = piece.n_units;
+    const int s = piece.s, kh = piece.kh, rg = piece.rg, rows = work.rows_of(s), n_units = piece.n_units;
     const int mine = n_units > warp ? (n_units - warp + W - 1) / W : 0;      // units warp, warp + W, ...
 
     // ---- queries: fp16 under a power of two of the row
@@ -358,7 +206,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
     }
 
     __syncwarp();
-    const Piece following = next_piece(piece.hi, piece.sk);
+    const I4Piece following = work.next_piece(piece.hi, piece.sk);
     if (following.n_units > 0) copy_queries(following);
     asm volatile("cp.async.commit_group;" ::: "memory");           // (older than the next unit's group: waited for with the unit before that)
 
@@ -460,7 +308,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
           for (int b = 0; b < SUBS; ++b) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const float e = i4_ex2((sT[b][nt][c] - m[nt][c & 1]) * sc[nt][c & 1]);
+              const float e = ex2((sT[b][nt][c] - m[nt][c & 1]) * sc[nt][c & 1]);
               sT[b][nt][c] = e;
               l[nt][c & 1] += e;
             }
@@ -543,7 +391,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
       }
     }
     __syncthreads();
-    const bool first = piece.first_page == 0, whole = first && (n_units >> upp_log) == piece.pages;
+    const bool first = piece.first_page == 0, whole = first && (n_units >> work.upp_log) == piece.pages;
     float* record = p.partials + static_cast<size_t>(blockIdx.x * 2 + (first ? 1 : 0)) * R * (D + 2);
     for (int i = tid; i < R * (D / 4); i += blockDim.x) {
       const int r = i / (D / 4), c = (i % (D / 4)) * 4;
@@ -567,80 +415,8 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
     }
     // the CTAs whose shares meet this segment are consecutive; the first of them leaves word for the kernel that merges their records
     if (first && tid == 0)
-      p.seg_records[piece.sk * p.n_rg + rg] = whole ? make_int2(0, 0) : segment_records(T, n_share, piece.seg_lo + p.pad, piece.seg_lo + p.pad + piece.pages);
+      p.seg_records[piece.sk * p.n_rg + rg] = whole ? make_int2(0, 0) : work.records(piece);
     piece = following;
     if (piece.n_units > 0) __syncthreads();          // the merge tile has been read
   }
-}
-
-// Segments that several CTAs share: a warp per row merges their records by log-sum-exp, in CTA order.
-constexpr int kI4CombineWarps = 4;
-template <int D, int R>
-__global__ void __launch_bounds__(kI4CombineWarps * 32) int4_combine_kernel(const __grid_constant__ I4Params p) {
-  grid_dep_wait();
-  const int lane = threadIdx.x & 31, w = blockIdx.x * kI4CombineWarps + (threadIdx.x >> 5);
-  const int seg = w / R, r = w % R;
-  if (seg >= p.n_sk * p.n_rg) return;
-  const int2 rec = p.seg_records[seg];
-  if (rec.y == 0) return;
-  const int sk = seg / p.n_rg, rg = seg - sk * p.n_rg, s = sk / p.Hkv, kh = sk - s * p.Hkv;
-  if (rg * R + r >= (p.n_active ? clamp_rows(p.n_active[s], p.B) : p.B) * p.G) return;
-  constexpr size_t kStep = static_cast<size_t>(2) * R * (D + 2);           // from a CTA's record to the next one's
-  constexpr int C = D / 32, kBatch = 8;
-  // the first CTA's record lies in its second place, the others' in their first
-  const float* first = p.partials + static_cast<size_t>(rec.x) * kStep;
-  float acc[C], M = -INFINITY, L = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = 0.f;
-  for (int b = 0; b < rec.y; b += kBatch) {
-    float m[kBatch], l[kBatch], x[kBatch][C];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int j = b + i;
-      m[i] = -INFINITY;
-      l[i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < C; ++c) x[i][c] = 0.f;
-      if (j < rec.y) {
-        const float* at = first + j * kStep + (j == 0 ? R * (D + 2) : 0);
-        m[i] = at[r];
-        l[i] = at[R + r];
-        if constexpr (C == 4) {
-          const float4 t = *reinterpret_cast<const float4*>(at + 2 * R + r * D + lane * 4);
-          x[i][0] = t.x; x[i][1] = t.y; x[i][2] = t.z; x[i][3] = t.w;
-        } else {
-          const float2 t = *reinterpret_cast<const float2*>(at + 2 * R + r * D + lane * 2);
-          x[i][0] = t.x; x[i][1] = t.y;
-        }
-      }
-    }
-    float top = M;
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, m[i]);
-    if (top == -INFINITY) continue;
-    const float keep = exp2f(M - top);
-    L *= keep;
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] *= keep;
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const float f = exp2f(m[i] - top);
-      L = fmaf(l[i], f, L);
-#pragma unroll
-      for (int c = 0; c < C; ++c) acc[c] = fmaf(x[i][c], f, acc[c]);
-    }
-    M = top;
-  }
-  const long long row = i4_row(p, s, kh, rg * R + r);
-  if (row < 0) return;
-  const bool empty = L == 0.f;
-  const float inv = empty ? 0.f : 4.f / L;
-  if constexpr (C == 4) {
-    i4_store4(p, row * D + lane * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-  } else {
-    // two columns a lane: pairs of lanes store four
-    const float o0 = __shfl_down_sync(0xffffffffu, acc[0], 1), o1 = __shfl_down_sync(0xffffffffu, acc[1], 1);
-    if ((lane & 1) == 0) i4_store4(p, row * D + lane * 2, acc[0] * inv, acc[1] * inv, o0 * inv, o1 * inv);
-  }
-  if (lane == 0 && p.lse) p.lse[row] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
 }

@@ -198,6 +198,17 @@ def test_bad_lists_tables_and_lengths_are_reported():
     c.check_all()
 
 
+@pytest.mark.parametrize("block,G", [(32, 4), (33, 4), (64, 16)])
+def test_expired_waits_end_with_a_status_and_the_context_stays_usable(block, G):
+    c = Cache([5000, 333], block=block, G=G)
+    c.ctx.set_wait_limit(1)
+    assert c.attn() == c.B.LOSA_ERR_TIMEOUT
+    assert c.ctx.poll_status() == 0
+    c.ctx.set_wait_limit(0)
+    assert c.attn() == 0
+    c.check_all()
+
+
 @pytest.mark.parametrize("block", [1, 4])
 def test_few_rows_wait_for_nothing_that_a_bound_could_end(block):
     c = Cache([5000, 333], block=block)
