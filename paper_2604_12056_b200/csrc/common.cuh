@@ -215,6 +215,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 }
 
 constexpr long long kWaitCycles = 2000000000ll;   // ~1 s: default bound of every mbarrier wait
+constexpr long long kLookCycles = 32;             // about what a look at a barrier takes
 constexpr long long kDrainCycles = 20000000ll;    // ~10 ms: bound of the waits for work already in flight when a CTA gives up
 // Bounded wait.  Returns false (and raises the CTA's abort flag) when the bound runs out or
 // another warp has already given up.

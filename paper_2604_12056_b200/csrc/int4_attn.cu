@@ -357,6 +357,10 @@ int32_t launch_tc(losa_ctx* c, I4Params p, cudaStream_t st) {
   auto kernel = int4_tc_kernel<D, GP>;
   if (!(c->int4_attr_set & 4)) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kI4SmemLimit));
+    // the kernel moves registers between its warps: a build that is launched with fewer than it deals out would wait for ever
+    cudaFuncAttributes fa;
+    LOSA_CUDA_TRY(c, cudaFuncGetAttributes(&fa, kernel));
+    if (fa.numRegs < kTcLaunchRegs) return LOSA_ERR_UNSUPPORTED;
     c->int4_attr_set |= 4;
   }
   static_assert(tc_smem<D>(kMaxSegments) <= kI4SmemLimit, "shared memory");
