@@ -31,6 +31,10 @@ template <int D> constexpr int tc_smem(int n_sk) {
   return 1024 + kTcRows * D * 2 + (kTcNK + kTcNV) * tc_tile<D>() + 512 + kTcMeta * 8 * 4 + (2 + 2 + 2) * kTcRows * 4 + (32 + n_sk + 1) * 4;
 }
 
+__device__ __forceinline__ void tc_store16(void* at, bool on, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p st.global.v4.b32 [%0], {%2, %3, %4, %5};\n\t}"
+               ::"l"(at), "r"(static_cast<int>(on)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -101,6 +105,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  __syncwarp();
   if (warp == 0) {                                   // tensor memory: taken while the previous kernel drains
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -118,9 +123,11 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
   if (!ok && any && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (ok) ok = warp_mbar_wait(bar, parity, abort_flag, p.status, p.wait_cycles);
+    __syncwarp();                                    // (what follows is for whole warps)
     return ok;
   };
 
+  __syncwarp();
   if (!any) {
   } else if (warp < kTcSoftWarps) {
     // ================================================================== softmax: thread = (set, query row)
@@ -128,7 +135,10 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
     const int set = warp >> 2, row = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_at = tmem + COL_S + set * 128 + lanes, o_at = tmem + COL_O + set * 128 + lanes;
-    auto all_meet = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kTcSoftWarps * 32) : "memory"); };
+    auto all_meet = [&]() {
+      __syncwarp();
+      asm volatile("bar.sync 1, %0;" ::"n"(kTcSoftWarps * 32) : "memory");
+    };
     I4Piece piece = work.next_piece(work.lo, work.sk0);
     int g = 0;                                       // groups before the piece
     float sc = 1.f;
@@ -273,6 +283,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
       const bool first = piece.first_page == 0, whole = first && (piece.n_units >> work.upp_log) == piece.pages;
       const int seg = piece.sk * p.n_rg + piece.rg, r = piece.rg * R + row;
       if (first && tid == 0) p.seg_records[seg] = whole ? make_int2(0, 0) : work.records(piece);
+      __syncwarp();
       if (!idle) {
         float* record = p.partials + static_cast<size_t>(blockIdx.x + seg) * (R * (D + 2));
         const long long out_row = r < work.rows_of(piece.s) ? i4_row(p, piece.s, piece.kh, r) : -1;
@@ -290,13 +301,23 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
             // column 8 j + (0 4 1 5 2 6 3 7)[i] of the result lies at 8 j + i
             x[(k & 8) + ((k & 7) >> 1) + (k & 1) * 4] = y0 + y1;
           }
-          if (out_row >= 0) {
+          // (stores under a predicate, not a branch: the loads of tensor memory around them need the whole warp)
+          if (!whole) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 4) {
-              if (whole) i4_store4(p, out_row * D + col + k, x[k] * inv, x[k + 1] * inv, x[k + 2] * inv, x[k + 3] * inv);
-              else *reinterpret_cast<float4*>(record + 2 * R + row * D + col + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-            }
+            for (int k = 0; k < 16; k += 4) tc_store16(record + 2 * R + row * D + col + k, out_row >= 0, __float_as_uint(x[k]), __float_as_uint(x[k + 1]), __float_as_uint(x[k + 2]), __float_as_uint(x[k + 3]));
+          } else if (p.out_bf16) {
+            auto pack = [&](int k) {
+              const __nv_bfloat162 t = __floats2bfloat162_rn(x[k] * inv, x[k + 1] * inv);
+              return *reinterpret_cast<const uint32_t*>(&t);
+            };
+#pragma unroll
+            for (int k = 0; k < 16; k += 8) tc_store16(static_cast<__nv_bfloat16*>(p.out) + out_row * D + col + k, out_row >= 0, pack(k), pack(k + 2), pack(k + 4), pack(k + 6));
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4)
+              tc_store16(static_cast<float*>(p.out) + out_row * D + col + k, out_row >= 0, __float_as_uint(x[k] * inv), __float_as_uint(x[k + 1] * inv), __float_as_uint(x[k + 2] * inv), __float_as_uint(x[k + 3] * inv));
           }
+          __syncwarp();
         }
         if (out_row >= 0 && set == 0) {
           if (whole) {
@@ -307,6 +328,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
           }
         }
       }
+      __syncwarp();
       tc5_fence_before();
       all_meet();                                      // (the exchange has been read)
       if (lane == 0) mbar_arrive(o_free, 1);
