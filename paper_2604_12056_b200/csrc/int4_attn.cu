@@ -375,7 +375,8 @@ int32_t launch_tc(losa_ctx* c, I4Params p, cudaStream_t st) {
   return after_launch(c);
 }
 
-// The kernel with the rows on the tensor cores' M side takes 1.x times the other one's for 16 rows (per pass of 16), and one pass does for 128.
+// Up to 16 rows the kernel on registers is the faster one (four tokens of four ragged 16K to 32K prompts, 16 rows: 52 us; the other one,
+// whose time does not depend on the rows, about 80), and for 17 to 32 it would pass over the cache twice.
 constexpr int kI4MmaRows = 16;
 template <int D, int GP>
 int32_t launch_rows(losa_ctx* c, I4Params p, cudaStream_t st) {

@@ -12,8 +12,6 @@
 //                 products of one run while the other is worked on), its own output and its own running maximum and sum: nothing
 //                 passes between the sets before a piece ends.  A row's 64 scores are read once and stay in registers; weights go
 //                 back over them as fp16.  The reference maximum only moves when it would grow by more than 2^8.
-//                 (Whole groups at a time, with the products, the softmax and the products of a set one after the other: 200 us where this
-//                 takes XXX; two passes over the scores: 202 us.)
 //   O[128 x D] += P V              another issuing warp; A = P from tensor memory, B = values as they lie (tokens x d); 4 instructions per half
 // Tensor memory is full: two outputs of D columns, two score tiles of 128.  Everything is handed on by mbarriers with bounded waits.
 #pragma once
@@ -105,22 +103,22 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  __syncwarp();
-  if (warp == 0) {                                   // tensor memory: taken while the previous kernel drains
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(512) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
   grid_dep_trigger();                                // (the merging kernel comes up beside this one)
   grid_dep_wait();
   I4Work<D, R> work(p, pre, runs, GP);
-  const bool any = work.begin(2 * PG);               // (meets all threads; shares of two groups at least)
+  if (!work.begin(2 * PG)) return;                   // (one answer for the CTA; shares of two groups at least)
+  __syncwarp();
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
   tc5_fence_before();
   __syncthreads();
   tc5_fence_after();
   const uint32_t tmem = warp_uniform(*tmem_slot);
   // a bound shorter than a look at a barrier takes has run out by then (which is how the way out is exercised)
   bool ok = p.wait_cycles >= kLookCycles;
-  if (!ok && any && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
+  if (!ok && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (ok) ok = warp_mbar_wait(bar, parity, abort_flag, p.status, p.wait_cycles);
     __syncwarp();                                    // (what follows is for whole warps)
@@ -128,8 +126,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
   };
 
   __syncwarp();
-  if (!any) {
-  } else if (warp < kTcSoftWarps) {
+  if (warp < kTcSoftWarps) {
     // ================================================================== softmax: thread = (set, query row)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcSoftRegs));
     const int set = warp >> 2, row = tid & 127;

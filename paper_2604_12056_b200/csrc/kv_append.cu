@@ -21,8 +21,13 @@ namespace losa {
 namespace {
 
 constexpr int kApWarps = 8, kApThreads = kApWarps * 32;
-constexpr int kApUnroll = 4;                       // rows (heads) of a lane in flight
 constexpr int kFmtNative = 0, kFmtFp8 = 1, kFmtInt4 = 2;
+// what a launch does: all of it, the pages, the queries (two launches, with the registers that each needs, where there is much to do)
+constexpr int kAll = 0, kPagesOnly = 1, kQueriesOnly = 2;
+// ... and the 16-byte pieces that a lane has in flight: of a page's rows (four, with the table's parts beside them, spill at three
+// blocks per SM: 32,768 tokens 226 us, 186 with two), of a token's heads.
+constexpr int kApRows = 2;
+constexpr int heads_in_flight(int role) { return role == kAll ? 4 : 8; }
 // where the new rows come from: the call's tokens, the pages of a bf16 cache, nowhere (summaries of what is there)
 constexpr int kSrcTokens = 0, kSrcPages = 1, kSrcNone = 2;
 
@@ -62,12 +67,14 @@ __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
   return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
 }
 
-// The part of a table row that a lane with elements j .. j + V - 1 of a head needs.
+// The part of a table row that a lane with elements j .. j + V - 1 of a head needs.  Always a load (of some row, where there is nothing to
+// rotate): one under a condition would be waited for on the spot, and the rows in flight came one after the other.
 template <int V> struct Turn { float c[V], s[V]; };
 template <int V>
 __device__ __forceinline__ Turn<V> load_turn(const AppendParams& p, int pos, int j) {
   Turn<V> t;
-  const size_t row = static_cast<size_t>(pos) * p.half;
+  const size_t row = static_cast<size_t>(min(max(pos, 0), p.n_pos - 1)) * p.half;
+  if (j >= 2 * p.half) j = 0;
   if (p.interleaved) {
     const float* c = p.cos_t + row + j / 2;
     const float* s = p.sin_t + row + j / 2;
@@ -86,8 +93,25 @@ __device__ __forceinline__ Turn<V> load_turn(const AppendParams& p, int pos, int
       t.c[i] = a.x; t.c[i + 1] = a.y; t.c[i + 2] = a.z; t.c[i + 3] = a.w;
       t.s[i] = b.x; t.s[i + 1] = b.y; t.s[i + 2] = b.z; t.s[i + 3] = b.w;
     }
+    if (j < p.half) {                                // the lower half takes its partner with a minus: x cos + (-sin) y
+#pragma unroll
+      for (int i = 0; i < V; ++i) t.s[i] = -t.s[i];
+    }
   }
   return t;
+}
+// Two products, two sums, each rounded by itself.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
 }
 // A lane's 16 bytes, rotated.  Products and sums are rounded one by one (no fused multiply-add): the result is that of the formula
 // as it is written, whatever the compiler would contract.  All lanes of the warp take part; `on`: this lane's elements are rotated.
@@ -110,11 +134,12 @@ __device__ __forceinline__ uint4 rotate(const AppendParams& p, const uint4& raw,
     o.w = __shfl_sync(0xffffffffu, raw.w, from);
     float z[V];
     unpack(o, z);
-    const bool lower = j < p.half;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float a = __fmul_rn(x[i], t.c[i]), b = __fmul_rn(z[i], t.s[i]);
-      y[i] = lower ? __fsub_rn(a, b) : __fadd_rn(a, b);
+    for (int i = 0; i < V; i += 2) {
+      const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(t.c[i], t.c[i + 1])), b = mul2(make_float2(z[i], z[i + 1]), make_float2(t.s[i], t.s[i + 1]));
+      const float2 r = add2(a, b);
+      y[i] = r.x;
+      y[i + 1] = r.y;
     }
   }
   return on ? pack(y) : raw;
@@ -183,9 +208,9 @@ __device__ __forceinline__ int find_seq(const int* first, int n, int i) {
 }
 
 // One page's new rows of one KV head and tensor.
-template <typename T, int FMT, int D, int SRC>
+template <typename T, int FMT, int D, int SRC, int U>
 __device__ __forceinline__ void append_page(const AppendParams& p, int s, int page, int kh, bool is_v, int lane) {
-  constexpr int V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR, U = kApUnroll;
+  constexpr int V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR;
   constexpr int RUNS = D / kInt4Run, LRUN = kInt4Run / V;        // 4-bit: runs per row, lanes per run
   const Span sp = span_of<SRC>(p, s);
   const int base = page * p.g;
@@ -222,68 +247,28 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
     }
     return raw;
   };
+  // the table's part for new row t; on: this lane's elements of it are to be rotated
   auto turn = [&](int t, bool here, bool& on) {
-    Turn<V> tn;
     on = here && j < 2 * p.half;
-    if (on) {
-      int pos = base + t;
-      if (p.pos) {
-        pos = p.pos[token_of(t)];
-        if (pos < 0 || pos >= p.n_pos) { on = false; set_status(p.status, LOSA_ERR_BOUNDS); }
-      }
-      if (on) tn = load_turn<V>(p, pos, j);
+    int pos = base + t;
+    if (p.pos) {
+      pos = here ? p.pos[token_of(t)] : 0;
+      if (pos < 0 || pos >= p.n_pos) { on = false; set_status(p.status, LOSA_ERR_BOUNDS); }
     }
-    if (!on) {
-#pragma unroll
-      for (int x = 0; x < V; ++x) { tn.c[x] = 1.f; tn.s[x] = 0.f; }
-    }
-    return tn;
-  };
-  auto rotated = [&](const uint4& raw, int t, bool here) {
-    bool on;
-    const Turn<V> tn = turn(t, here, on);
-    return rotate<T, V>(p, raw, tn, j, on, lane);
+    return load_turn<V>(p, pos, j);
   };
   auto out_row = [&](int t) { return reinterpret_cast<uint4*>(keep + (static_cast<size_t>(token_of(t)) * p.Hkv + kh) * D + j); };
 
   if constexpr (FMT == kFmtFp8) {
-    // one scale for the page: its old rows and the new ones are gone over twice, for the largest value and for the codes (the second
-    // time they come from the caches)
+    // one scale for the page, from its old rows and the new ones together.  A page whose slice a warp can hold (16 pieces per lane) is requested
+    // as a whole and stays in registers; a larger one is gone over twice, for the largest value and for the codes (the second time it
+    // comes from the caches).  That takes 200 registers, one block per SM, and is faster at every size all the same: eight blocks of 32 tokens
+    // 16 us, all twice at two blocks per SM 22.6; 18,000 tokens 164 and 223; 64 single tokens 16.8 and 26.1.
+    constexpr int M = 16;
     const float old_scale = *page_scale;
-    auto old_row = [&](int t) {
-      float v[8];
-      fp8_decode8(*reinterpret_cast<const uint2*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j), v);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[x] *= old_scale;
-      return pack(v);                                // exact: four significant bits
-    };
-    auto value = [&](int t) {                        // all lanes
-      const bool here = t >= t_lo && t < t_hi;
-      uint4 raw = fetch(t, here);
-      if (rot) raw = rotated(raw, t, here);
-      if (t < t_lo) raw = old_row(t);
-      return raw;
-    };
-#pragma unroll 2
-    for (int tb = 0; tb < t_hi; tb += RPI) {
-      const int t = tb + sub;
-      const uint4 raw = value(t);
-      if (t < t_hi) {
-        float v[8];
-        unpack(raw, v);
-        extremes(v);
-      }
-    }
-    float amax = 0.f;
-#pragma unroll
-    for (int x = 0; x < V; ++x)
-      if (lo[x] <= hi[x]) amax = fmaxf(amax, fmaxf(fabsf(lo[x]), fabsf(hi[x])));
-    const int e = fp8_scale_exp(warp_max(amax));
-    const float scale = pow2f(e), inv = pow2f(-e);
-#pragma unroll 2
-    for (int tb = 0; tb < p.g; tb += RPI) {
-      const int t = tb + sub;
-      const uint4 raw = value(t);
+    const bool held = p.g <= M * RPI;
+    uint4 all[M];
+    auto encode = [&](int t, const uint4& raw, float scale, float inv) {
       float v[8];
       unpack(raw, v);
       const uint2 code = t < t_hi ? fp8_encode8(v, inv) : make_uint2(0u, 0u);
@@ -294,6 +279,97 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
 #pragma unroll
         for (int x = 0; x < 8; ++x) w[x] *= scale;
         *out_row(t) = pack(w);
+      }
+    };
+    auto old_row = [&](uint2 codes) {
+      float v[8];
+      fp8_decode8(codes, v);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] *= old_scale;
+      return pack(v);                                // exact: four significant bits
+    };
+    constexpr int F = 2;                             // rows in flight
+    auto values = [&](int tb, uint4 (&raw)[F]) {     // all lanes
+#pragma unroll
+      for (int u = 0; u < F; ++u) {
+        const int t = tb + u * RPI + sub;
+        raw[u] = fetch(t, t >= t_lo && t < t_hi);
+      }
+      uint2 old[F];
+      Turn<V> tn[F];
+      bool on[F];
+      if (rot) {
+#pragma unroll
+        for (int u = 0; u < F; ++u) tn[u] = turn(tb + u * RPI + sub, tb + u * RPI + sub >= t_lo && tb + u * RPI + sub < t_hi, on[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < F; ++u) {
+        const int t = tb + u * RPI + sub;
+        old[u] = t < t_lo ? *reinterpret_cast<const uint2*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j) : make_uint2(0u, 0u);
+      }
+#pragma unroll
+      for (int u = 0; u < F; ++u) {
+        const int t = tb + u * RPI + sub;
+        if (rot) raw[u] = rotate<T, V>(p, raw[u], tn[u], j, on[u], lane);
+        if (t < t_lo) raw[u] = old_row(old[u]);
+      }
+    };
+    if (held) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        const int t = i * RPI + sub;
+        all[i] = fetch(t, t >= t_lo && t < t_hi);
+      }
+      for (int tb = 0; tb < t_lo; tb += RPI) {       // (few pages have old rows)
+        const int t = tb + sub;
+        const uint2 codes = t < t_lo ? *reinterpret_cast<const uint2*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          if (i * RPI == tb && t < t_lo) all[i] = old_row(codes);
+      }
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        const int t = i * RPI + sub;
+        if (rot && i * RPI < t_hi && i * RPI + RPI > t_lo) {
+          bool on;
+          const Turn<V> tn = turn(t, t >= t_lo && t < t_hi, on);
+          all[i] = rotate<T, V>(p, all[i], tn, j, on, lane);
+        }
+        if (t < t_hi) {
+          float v[8];
+          unpack(all[i], v);
+          extremes(v);
+        }
+      }
+    } else {
+      for (int tb = 0; tb < t_hi; tb += RPI * F) {
+        uint4 raw[F];
+        values(tb, raw);
+#pragma unroll
+        for (int u = 0; u < F; ++u)
+          if (tb + u * RPI + sub < t_hi) {
+            float v[8];
+            unpack(raw[u], v);
+            extremes(v);
+          }
+      }
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int x = 0; x < V; ++x)
+      if (lo[x] <= hi[x]) amax = fmaxf(amax, fmaxf(fabsf(lo[x]), fabsf(hi[x])));
+    const int e = fp8_scale_exp(warp_max(amax));
+    const float scale = pow2f(e), inv = pow2f(-e);
+    if (held) {
+#pragma unroll
+      for (int i = 0; i < M; ++i)
+        if (i * RPI + sub < p.g) encode(i * RPI + sub, all[i], scale, inv);
+    } else {
+      for (int tb = 0; tb < p.g; tb += RPI * F) {
+        uint4 raw[F];
+        values(tb, raw);
+#pragma unroll
+        for (int u = 0; u < F; ++u) encode(tb + u * RPI + sub, raw[u], scale, inv);
       }
     }
     __syncwarp();                                    // every lane has read the old scale
@@ -307,6 +383,9 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
       for (int x = 0; x < 8; ++x) { lo[x] = a[x] * scale; hi[x] = b[x] * scale; }
     }
   } else {
+    uint4 raw[U];                                    // the first rows are requested before those of the page that were there
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = fetch(t_lo + u * RPI + sub, t_lo + u * RPI + sub < t_hi);
     if (summaries)                                   // rows that were there before
       for (int t = sub; t < t_lo; t += RPI) {
         float v[V];
@@ -319,14 +398,22 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
         extremes(v);
       }
     for (int tb = t_lo; tb < t_hi; tb += RPI * U) {
-      uint4 raw[U];
+      if (tb > t_lo) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = fetch(tb + u * RPI + sub, tb + u * RPI + sub < t_hi);
+        for (int u = 0; u < U; ++u) raw[u] = fetch(tb + u * RPI + sub, tb + u * RPI + sub < t_hi);
+      }
+      if (rot) {
+        Turn<V> tn[U];
+        bool on[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) tn[u] = turn(tb + u * RPI + sub, tb + u * RPI + sub < t_hi, on[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = rotate<T, V>(p, raw[u], tn[u], j, on[u], lane);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int t = tb + u * RPI + sub;
         const bool here = t < t_hi;
-        if (rot) raw[u] = rotated(raw[u], t, here);
         float v[V];
         unpack(raw[u], v);
         if constexpr (FMT == kFmtInt4) {
@@ -376,10 +463,18 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
 }
 
 // Rotated heads h0 .. of one token, out of place or in place.
-template <typename T, int D>
+template <typename T, int D, int U>
 __device__ __forceinline__ void rotate_token(const AppendParams& p, int t, int h0, const void* x, int64_t stride, void* out, int H, int lane) {
-  constexpr int V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR, U = kApUnroll;
+  constexpr int V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR;
   const int sub = lane / LPR, j = (lane % LPR) * V;
+  const T* src = static_cast<const T*>(x) + static_cast<int64_t>(t) * stride + j;
+  T* dst = static_cast<T*>(out) + static_cast<size_t>(t) * H * D + j;
+  uint4 raw[U];                                      // requested before it is known where the token belongs
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int h = h0 + u * RPI + sub;
+    raw[u] = h < H ? *reinterpret_cast<const uint4*>(src + h * D) : make_uint4(0u, 0u, 0u, 0u);
+  }
   int pos = 0;
   if (p.pos) {
     pos = p.pos[t];
@@ -392,21 +487,8 @@ __device__ __forceinline__ void rotate_token(const AppendParams& p, int t, int h
   }
   bool on = j < 2 * p.half;
   if (p.half > 0 && (pos < 0 || pos >= p.n_pos)) { on = false; set_status(p.status, LOSA_ERR_BOUNDS); }
-  const T* src = static_cast<const T*>(x) + static_cast<int64_t>(t) * stride + j;
-  T* dst = static_cast<T*>(out) + static_cast<size_t>(t) * H * D + j;
-  uint4 raw[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int h = h0 + u * RPI + sub;
-    raw[u] = h < H ? *reinterpret_cast<const uint4*>(src + h * D) : make_uint4(0u, 0u, 0u, 0u);
-  }
   Turn<V> tn;
-  if (on) {
-    tn = load_turn<V>(p, pos, j);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) { tn.c[i] = 1.f; tn.s[i] = 0.f; }
-  }
+  if (p.half > 0) tn = load_turn<V>(p, pos, j);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int h = h0 + u * RPI + sub;
@@ -415,17 +497,17 @@ __device__ __forceinline__ void rotate_token(const AppendParams& p, int t, int h
   }
 }
 
-template <typename T, int FMT, int D, int SRC>
-__global__ void __launch_bounds__(kApThreads) append_kernel(AppendParams p) {
+template <typename T, int FMT, int D, int SRC, int ROLE>
+__global__ void __launch_bounds__(kApThreads, FMT == kFmtFp8 && SRC == kSrcTokens ? 1 : ROLE == kAll ? 2 : 3) append_kernel(const __grid_constant__ AppendParams p) {
   extern __shared__ int pre[];                       // [N + 1]
   grid_dep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool stored = p.k_pages != nullptr;
-  if (stored) {
+  if (stored && ROLE != kQueriesOnly) {
     if (warp == 0) page_prefix<SRC>(p, pre, lane);
     __syncthreads();
   }
-  if (SRC == kSrcTokens && blockIdx.x == 0) {
+  if (SRC == kSrcTokens && ROLE != kQueriesOnly && blockIdx.x == 0) {
     for (int s = threadIdx.x; s < p.N && (p.kv_len_out || !stored); s += kApThreads) {
       if (!stored && p.pos) break;
       const Span sp = span_of<SRC>(p, s);
@@ -433,38 +515,48 @@ __global__ void __launch_bounds__(kApThreads) append_kernel(AppendParams p) {
       else if (sp.n > 0 && stored) p.kv_len_out[s] = sp.a + sp.n;
     }
   }
-  constexpr int RPI = 32 / (D / vec_of<T>()), HEADS = RPI * kApUnroll;      // heads of a token that a unit takes
+  constexpr int RPI = 32 / (D / vec_of<T>()), QU = heads_in_flight(ROLE), HEADS = RPI * QU;      // heads of a token that a unit takes
   const int tensors = SRC == kSrcNone ? 1 : 2;
-  const long long page_units = stored ? static_cast<long long>(pre[p.N]) * tensors * p.Hkv : 0;
-  const int q_runs = SRC == kSrcTokens && p.q_out ? (p.Hq + HEADS - 1) / HEADS : 0;
-  const int k_runs = SRC == kSrcTokens && !stored && p.k_out ? (p.Hkv + HEADS - 1) / HEADS : 0;
+  const long long page_units = stored && ROLE != kQueriesOnly ? static_cast<long long>(pre[p.N]) * tensors * p.Hkv : 0;
+  const int q_runs = SRC == kSrcTokens && ROLE != kPagesOnly && p.q_out ? (p.Hq + HEADS - 1) / HEADS : 0;
+  const int k_runs = SRC == kSrcTokens && ROLE != kPagesOnly && !stored && p.k_out ? (p.Hkv + HEADS - 1) / HEADS : 0;
   const long long units = page_units + static_cast<long long>(p.T) * (q_runs + k_runs);
   for (long long u = static_cast<long long>(blockIdx.x) * kApWarps + warp; u < units; u += static_cast<long long>(gridDim.x) * kApWarps) {
-    if (u < page_units) {
+    if (ROLE != kQueriesOnly && u < page_units) {
       const int item = static_cast<int>(u / (tensors * p.Hkv)), rest = static_cast<int>(u % (tensors * p.Hkv));
       const int s = find_seq(pre, p.N, item);
       const int first_page = SRC == kSrcTokens ? p.start[s] / p.g : 0;
-      append_page<T, FMT, D, SRC>(p, s, first_page + item - pre[s], rest % p.Hkv, rest >= p.Hkv, lane);
-    } else if constexpr (SRC == kSrcTokens) {
+      append_page<T, FMT, D, SRC, kApRows>(p, s, first_page + item - pre[s], rest % p.Hkv, rest >= p.Hkv, lane);
+    } else if constexpr (SRC == kSrcTokens && ROLE != kPagesOnly) {
       const long long v = u - page_units;
       const int t = static_cast<int>(v / (q_runs + k_runs)), r = static_cast<int>(v % (q_runs + k_runs));
-      if (r < q_runs) rotate_token<T, D>(p, t, r * HEADS, p.q, p.q_stride, p.q_out, p.Hq, lane);
-      else rotate_token<T, D>(p, t, (r - q_runs) * HEADS, p.k, p.k_stride, p.k_out, p.Hkv, lane);
+      if (r < q_runs) rotate_token<T, D, QU>(p, t, r * HEADS, p.q, p.q_stride, p.q_out, p.Hq, lane);
+      else rotate_token<T, D, QU>(p, t, (r - q_runs) * HEADS, p.k, p.k_stride, p.k_out, p.Hkv, lane);
     }
   }
 }
 
 // `units`: at most so many
-template <typename T, int FMT, int D, int SRC>
+template <typename T, int FMT, int D, int SRC, int ROLE>
 int32_t launch_units(losa_ctx* c, const AppendParams& p, long long units, cudaStream_t st) {
   if (units <= 0) return LOSA_OK;
   const long long blocks = std::min<long long>((units + kApWarps - 1) / kApWarps, static_cast<long long>(c->n_sms) * 8);
-  launch_streaming(append_kernel<T, FMT, D, SRC>, static_cast<unsigned>(blocks), kApThreads, (p.N + 1) * sizeof(int), st, p);
+  launch_streaming(append_kernel<T, FMT, D, SRC, ROLE>, static_cast<unsigned>(blocks), kApThreads, (p.N + 1) * sizeof(int), st, p);
   return after_launch(c);
 }
-template <typename T, int FMT, int SRC>
+template <typename T, int FMT, int SRC, int ROLE = kAll>
 int32_t launch_dim(losa_ctx* c, const AppendParams& p, long long units, cudaStream_t st) {
-  return c->shape.head_dim == 128 ? launch_units<T, FMT, 128, SRC>(c, p, units, st) : launch_units<T, FMT, 64, SRC>(c, p, units, st);
+  return c->shape.head_dim == 128 ? launch_units<T, FMT, 128, SRC, ROLE>(c, p, units, st) : launch_units<T, FMT, 64, SRC, ROLE>(c, p, units, st);
+}
+// From so many bytes of queries on, queries and pages are two launches.
+constexpr long long kSplitBytes = 8ll << 20;
+template <typename T, int FMT>
+int32_t launch_tokens(losa_ctx* c, const AppendParams& p, long long pages, long long tokens, cudaStream_t st) {
+  if (p.k_pages && p.q_out && tokens * p.Hq * c->shape.head_dim * static_cast<long long>(sizeof(T)) >= kSplitBytes) {
+    const int32_t rc = launch_dim<T, FMT, kSrcTokens, kPagesOnly>(c, p, pages * 2 * p.Hkv, st);
+    return rc != LOSA_OK ? rc : launch_dim<T, kFmtNative, kSrcTokens, kQueriesOnly>(c, p, tokens * p.Hq, st);
+  }
+  return launch_dim<T, FMT, kSrcTokens>(c, p, pages * 2 * p.Hkv + tokens * (p.Hq + p.Hkv), st);
 }
 
 AppendParams base_params(const losa_ctx* c, const losa_kv_t* kv) {
@@ -514,12 +606,12 @@ int32_t launch_rope_append(losa_ctx* c, losa_kv_t* kv, const losa_rope_t* rope, 
   p.T = tk->n_tokens;
   // a sequence's tokens touch one page more than they fill at most, and no more pages than there are tokens
   const long long pages = std::min<long long>(p.T, p.T / sh.page_size + 2ll * sh.batch);
-  const long long units = (kv ? pages * 2 * p.Hkv : 0) + static_cast<long long>(p.T) * (p.Hq + p.Hkv);
-  if (sh.dtype == LOSA_F32) return launch_dim<float, kFmtNative, kSrcTokens>(c, p, units, st);
+  const long long stored = kv ? pages : 0;
+  if (sh.dtype == LOSA_F32) return launch_tokens<float, kFmtNative>(c, p, stored, p.T, st);
   const int fmt = kv ? kv->kv_format : LOSA_KV_NATIVE;
-  if (fmt == LOSA_KV_FP8_E4M3) return launch_dim<__nv_bfloat16, kFmtFp8, kSrcTokens>(c, p, units, st);
-  if (fmt == LOSA_KV_INT4) return launch_dim<__nv_bfloat16, kFmtInt4, kSrcTokens>(c, p, units, st);
-  return launch_dim<__nv_bfloat16, kFmtNative, kSrcTokens>(c, p, units, st);
+  if (fmt == LOSA_KV_FP8_E4M3) return launch_tokens<__nv_bfloat16, kFmtFp8>(c, p, stored, p.T, st);
+  if (fmt == LOSA_KV_INT4) return launch_tokens<__nv_bfloat16, kFmtInt4>(c, p, stored, p.T, st);
+  return launch_tokens<__nv_bfloat16, kFmtNative>(c, p, stored, p.T, st);
 }
 
 // the kv_len / step counters are bumped by the caller's counter kernel afterwards
