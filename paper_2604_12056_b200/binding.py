@@ -177,14 +177,17 @@ def make_rope(cos, sin, interleaved=False) -> RopeT:
 
 def make_new_tokens(q, k, v, cu, start, pos=None, q_out=None, k_out=None, v_out=None) -> NewTokensT:
     """losa_new_tokens_t over [T, H, d] tensors whose heads are contiguous within a token's row (the rows may lie
-    anywhere, as parts of a packed projection do); any of q, k, v may be None where the call does not need it."""
+    anywhere, as parts of a packed projection do); any of q, k, v may be None where the call does not need it.  The
+    outputs are contiguous, of any shape with as many elements."""
     T, strides = 0, []
     for t in (q, k, v):
         if t is not None:
             assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
             T = t.shape[0]
         strides.append(0 if t is None else t.stride(0) if T > 1 else t.shape[1] * t.shape[2])
-    assert all(t is None or t.shape[0] == T for t in (q, k, v, q_out, k_out, v_out)) and (pos is None or pos.numel() == T)
+    assert all(t is None or t.shape[0] == T for t in (q, k, v)) and (pos is None or pos.numel() == T)
+    for out, of in ((q_out, q), (k_out, k), (v_out, v)):
+        assert out is None or (of is not None and out.numel() == of.numel() and out.dtype == of.dtype)
     assert all(t is None or t.dtype == torch.int32 for t in (cu, start, pos))
     ptr = [None if t is None else t.data_ptr() for t in (q, k, v)]
     n = NewTokensT(*ptr, *strides, _ptr(cu), _ptr(start), _ptr(pos), T, _ptr(q_out), _ptr(k_out), _ptr(v_out))
