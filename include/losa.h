@@ -144,8 +144,8 @@ int32_t losa_destroy(losa_ctx* ctx);
  * (LOSA_ERR_TIMEOUT or LOSA_ERR_BOUNDS) and clears it, or LOSA_OK. */
 int32_t losa_poll_status(losa_ctx* ctx, void* stream);
 
-/* Bound of the waits inside the bf16 stage-4 kernel (its warps hand work to one another through
- * shared-memory barriers), in SM clock cycles; `cycles` <= 0 restores the default of about one
+/* Bound of the waits inside the bf16 stage-4 kernel and the kernel for more than 16 query rows per KV
+ * head over 4-bit pages (their warps hand work to one another through shared-memory barriers), in SM clock cycles; `cycles` <= 0 restores the default of about one
  * second.  A wait that outlasts the bound makes its thread block record LOSA_ERR_TIMEOUT, wait
  * (again within a bound) for the page copies and tensor-core instructions it had already started,
  * release its tensor memory and return: the launch ends normally, the step's results are

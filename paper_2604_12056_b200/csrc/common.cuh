@@ -74,6 +74,7 @@ struct losa_ctx {
   int32_t approx_attr_set;
   int32_t refine_attr_set;
   int32_t int4_attr_set;     // and for the 4-bit attention kernels, a bit each
+  int32_t append_attr_set;   // and for the FP8 append kernel, by role
   // optional timing of the stage-4 main kernel
   int32_t profile;
   cudaEvent_t ev_begin, ev_end;

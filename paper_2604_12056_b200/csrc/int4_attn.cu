@@ -26,7 +26,7 @@ struct I4Params {
   float* partials;
   int2* seg_records;                                // per segment: first CTA and number of its records (0: none to merge)
   int32_t* status;
-  int N, B, Hq, Hkv, G, g, Pmax, n_phys, n_sk, n_rg, min_units, pad;
+  int N, B, Hq, Hkv, G, g, Pmax, n_phys, n_sk, n_rg, pad;
   int rows_above, rows_upto;                       // segments with as many query rows are this kernel's
   float sm_scale;
   long long wait_cycles;                           // bound of every mbarrier wait, in SM clock cycles
@@ -328,23 +328,23 @@ int mma_smem(int warps, int stages, int ut, int n_sk) {
 template <int D, int NT, int UT>
 int32_t launch_mma(losa_ctx* c, I4Params p, int max_rows, cudaStream_t st) {
   constexpr int R = 8 * NT;
-  constexpr int S = 2;
-  auto kernel = int4_mma_kernel<D, NT, UT, S>;
+  auto kernel = int4_mma_kernel<D, NT, UT>;
   const int bit = NT;        // a context has one head dimension and one page size
   if (!(c->int4_attr_set & bit)) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kI4SmemLimit));
     c->int4_attr_set |= bit;
   }
   p.n_rg = (max_rows + R - 1) / R;
-  // Few segments: one CTA of all warps per SM.  More segments than SMs: CTAs of four warps, whose ends and starts overlap.
+  // Few segments: one CTA of all warps per SM.  More segments than SMs: CTAs of four warps, whose ends and starts overlap.  One token each,
+  // large and small CTAs: 8 segments of 8,192 tokens 14.2 and 15.6 us, 64 of 32,768 76.6 and 76.7, 496 of up to 4,095 67.8 and 62.8.
+  // The pads are pages that a CTA reads in the time that entering a segment takes; 12 instead of 24 for the large CTAs: 94.9 instead of 67.8.
   const bool many = p.n_sk * p.n_rg > c->n_sms;
   const int W = many ? 4 : i4_warps(NT), per_sm = many ? i4_warps(NT) / 4 : 1;
-  p.min_units = 1;
   p.pad = many ? 10 : 24;
   int grid = c->n_sms * per_sm;
   grid = std::min<long long>(grid, static_cast<long long>(c->lay.n_slots) * kRowsPerGroup / (2 * R));      // room for the records
   if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
-  launch_k(kernel, grid, W * 32, mma_smem<D, NT>(W, S, UT, p.n_sk), st, p);
+  launch_k(kernel, grid, W * 32, mma_smem<D, NT>(W, kI4Ring, UT, p.n_sk), st, p);
   if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
   const int32_t rc = after_launch(c);
   if (rc != LOSA_OK) return rc;
@@ -375,8 +375,9 @@ int32_t launch_tc(losa_ctx* c, I4Params p, cudaStream_t st) {
   return after_launch(c);
 }
 
-// Up to 16 rows the kernel on registers is the faster one (four tokens of four ragged 16K to 32K prompts, 16 rows: 52 us; the other one,
-// whose time does not depend on the rows, about 80), and for 17 to 32 it would pass over the cache twice.
+// Up to 16 rows the kernel on registers is the faster one, whose time grows with every pass of 16 rows; the other's does not depend on the
+// rows.  Registers and tensor memory, 16 rows: eight prompts of 32,768 tokens 104 and 175 us, four of 16K to 32K 52 and 78, 64 of
+// about 1,400 81 and 93, one of 8,201 18.1 and 18.6.  32 rows: 194 and 175, 90 and 78, 164 and 94, 21.0 and 20.3.
 constexpr int kI4MmaRows = 16;
 template <int D, int GP>
 int32_t launch_rows(losa_ctx* c, I4Params p, cudaStream_t st) {

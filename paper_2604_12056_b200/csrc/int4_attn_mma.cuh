@@ -1,7 +1,8 @@
 // Attention over 4-bit pages, up to 16 query rows per pass: included by int4_attn.cu (same namespace).
 //
-// The cache's bytes bound this kernel (68 per row of 128), and right behind them the instructions that turn codes into
-// operands.  So tokens, not query rows, are the M side of every product, codes become operands in registers, and
+// What it cannot do without are the cache's bytes (68 per row of 128); what bounds it are the instructions that turn codes into
+// operands: about 640 per unit of 32 tokens, issued at 2.5 a cycle and SM.  Eight prompts of 32,768 tokens, one token each (8 rows per KV
+// head): 76 us, 58 % of the copy rate; 16 rows 104; one prompt of 8,192 14.2, most of it latency.  So tokens, not query rows, are the M side of every product, codes become operands in registers, and
 // nothing but codes passes through shared memory:
 //   S^T[16 tokens x 8 rows] += K[16 x 16 d] Q^T[16 d x 8]     mma.sync.m16n8k16, A = keys: a lane takes the quarter
 //                                (d/4 elements, 16 bytes at d = 128) of two rows that lies in one piece; which elements the
@@ -24,6 +25,7 @@ constexpr int i4_warps(int nt) { return nt == 1 ? 12 : 8; }     // most warps of
 template <int D> constexpr int i4_unit_codes(int ut) { return ut * D; }          // bytes of a unit's codes, K and V
 template <int D> constexpr int i4_unit_scales(int ut) { return ut * D / 16; }    // ... and scales
 template <int D, int NT> constexpr int i4_merge_bytes(int warps) { return ((warps * 8 * NT * (D + 4) * 4 + warps * 8 * NT * 8) + 15) / 16 * 16; }
+constexpr int kI4Ring = 2;                          // units of a ring
 constexpr int kI4Stride = 4;                        // floats between the rows of the merge tile: a row is D + 4
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -58,11 +60,11 @@ __device__ __forceinline__ void i4_copy4(uint32_t dst, const uint8_t* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// UT: tokens of a unit, S: units of a ring
-template <int D, int NT, int UT, int S>
+// UT: tokens of a unit
+template <int D, int NT, int UT>
 __global__ void __launch_bounds__(i4_warps(NT) * 32, 1)
 int4_mma_kernel(const __grid_constant__ I4Params p) {
-  constexpr int R = 8 * NT, KS = D / 16, MT = D / 16, E = D / 8, WL = D / 32, RUNS = D / kInt4Run;
+  constexpr int S = kI4Ring, R = 8 * NT, KS = D / 16, MT = D / 16, E = D / 8, WL = D / 32, RUNS = D / kInt4Run;
   constexpr int UC = i4_unit_codes<D>(UT), US = i4_unit_scales<D>(UT), SUBS = UT / 16;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -84,7 +86,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
   grid_dep_wait();
   // no more shares than give every warp a unit
   I4Work<D, R> work(p, pre, chunk_s, UT);
-  if (!work.begin(W * p.min_units)) return;
+  if (!work.begin(W)) return;
   // ---- the ring: units warp, warp + W, ... of every piece, one piece after the other; the copies run S - 1 units ahead
   unsigned long long policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -359,18 +361,17 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
       __syncwarp();                                  // the slot has been read
     };
     // slots in turn, known at compile time: addresses are then one register and an offset
+    static_assert(S == 2, "two slots");
     int k = 0;
-    if constexpr (S == 2) {
-      if (mine > 0 && next_slot == 1) { take(std::integral_constant<int, 1>{}); ++k; }
+    if (mine > 0 && next_slot == 1) { take(std::integral_constant<int, 1>{}); ++k; }
 #pragma unroll 1
-      for (; k + 2 <= mine; k += 2) {
-        take(std::integral_constant<int, 0>{});
-        take(std::integral_constant<int, 1>{});
-      }
-      next_slot = 0;
-      if (k < mine) { take(std::integral_constant<int, 0>{}); next_slot = 1; }
-      if (mine == 0) next_slot = next_slot_was;
+    for (; k + 2 <= mine; k += 2) {
+      take(std::integral_constant<int, 0>{});
+      take(std::integral_constant<int, 1>{});
     }
+    next_slot = 0;
+    if (k < mine) { take(std::integral_constant<int, 0>{}); next_slot = 1; }
+    if (mine == 0) next_slot = next_slot_was;
 
     // ---- merge of the CTA's warps
 #pragma unroll

@@ -4,7 +4,7 @@
 // cores, 128 query rows at a time (one per tensor-memory lane), and the cache is turned into fp16 operands once for
 // all of them.  Pages are taken in groups of 128 tokens:
 //   eight warps   turn codes into fp16 tiles in shared memory (32 tokens each, four warps for keys and four for values): 16 bytes of
-//                 codes and their scale from global memory into registers a group ahead, four 16-byte stores of swizzled chunks; the
+//                 codes and their scale from global memory into registers a group ahead (L2: sixteen), four 16-byte stores of swizzled chunks; the
 //                 eight elements of a chunk lie in the order 0 4 1 5 2 6 3 7 in which the conversion yields them, and so do
 //                 the queries' and the output's columns
 //   S[128 x 64] = Q K^T            an issuing warp; A = Q, B = half a group's keys, both from shared memory; D / 16 instructions
@@ -13,6 +13,8 @@
 //                 passes between the sets before a piece ends.  A row's 64 scores are read once and stay in registers; weights go
 //                 back over them as fp16.  The reference maximum only moves when it would grow by more than 2^8.
 //   O[128 x D] += P V              another issuing warp; A = P from tensor memory, B = values as they lie (tokens x d); 4 instructions per half
+// A block of 32 tokens (128 rows) over eight prompts of 32,768: 183 us, 46 % of the products' own time at the dense bf16 rate; the products and
+// their barriers alone take 132, since an operand in shared memory is read again by every instruction.
 // Tensor memory is full: two outputs of D columns, two score tiles of 128.  Everything is handed on by mbarriers with bounded waits.
 #pragma once
 

@@ -2,7 +2,7 @@
 // summaries (losa_rope_append); the same pass without rotation appends a finished block to 4-bit pages, turns a bf16
 // cache into 4-bit pages and summarises 4-bit pages.
 //
-// A copy with a little arithmetic on the way, so HBM bounds it, and a chain of dependent reads (lengths, page table,
+// A copy with a little arithmetic on the way, so HBM bounds it (32,768 tokens of 32 / 8 heads x 128, bf16: 184 us, 70 % of the copy rate), and a chain of dependent reads (lengths, page table,
 // rows) when there are few tokens.  Work is cut into units of one warp each, handed out over a flat list, so ragged
 // batches leave no warp idle and empty sequences cost nothing:
 //   (touched page, tensor, KV head)   the new rows of a page: 16 bytes of a row per lane, four loads in flight,
@@ -27,6 +27,14 @@ constexpr int kAll = 0, kPagesOnly = 1, kQueriesOnly = 2;
 // ... and the 16-byte pieces that a lane has in flight: of a page's rows (four, with the table's parts beside them, spill at three
 // blocks per SM: 32,768 tokens 226 us, 186 with two), of a token's heads.
 constexpr int kApRows = 2;
+// 16-byte pieces per lane of an FP8 page that a warp holds in shared memory
+constexpr int kApHeld = 16;
+constexpr int kApHeldBytes = kApWarps * kApHeld * 32 * 16;
+// FP8 pages: two rows' parts of the table in flight and one block per SM in the one launch (few pages: latency), one and two blocks in a launch of
+// its own (many).  64 / 1,024 / 2,048 / 8,192 tokens in one launch: 12.1 / 16.9 / 27.1 / 79.8 us the first way, 16.0 / 17.2 / 22.0 / 69.5 the
+// second; three blocks in a launch of its own: 86.4 instead of 69.4.
+constexpr int fp8_rows(int role) { return role == kAll ? 2 : 1; }
+constexpr int blocks_per_sm(int fmt, int role) { return (role == kAll ? 2 : 3) - (fmt == kFmtFp8 ? 1 : 0); }
 constexpr int heads_in_flight(int role) { return role == kAll ? 4 : 8; }
 // where the new rows come from: the call's tokens, the pages of a bf16 cache, nowhere (summaries of what is there)
 constexpr int kSrcTokens = 0, kSrcPages = 1, kSrcNone = 2;
@@ -207,10 +215,13 @@ __device__ __forceinline__ int find_seq(const int* first, int n, int i) {
   return a;
 }
 
-// One page's new rows of one KV head and tensor.
-template <typename T, int FMT, int D, int SRC, int U>
-__device__ __forceinline__ void append_page(const AppendParams& p, int s, int page, int kh, bool is_v, int lane) {
-  constexpr int V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR;
+__device__ __forceinline__ void copy_async16(uint4* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src) : "memory");
+}
+// One page's new rows of one KV head and tensor; hold: this lane's first piece of kApHeld, 32 apart (FP8 pages).
+template <typename T, int FMT, int D, int SRC, int ROLE>
+__device__ __forceinline__ void append_page(const AppendParams& p, int s, int page, int kh, bool is_v, uint4* hold, int lane) {
+  constexpr int U = kApRows, V = vec_of<T>(), LPR = D / V, RPI = 32 / LPR;
   constexpr int RUNS = D / kInt4Run, LRUN = kInt4Run / V;        // 4-bit: runs per row, lanes per run
   const Span sp = span_of<SRC>(p, s);
   const int base = page * p.g;
@@ -235,18 +246,12 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
   };
   auto token_of = [&](int t) { return sp.first + base + t - sp.a; };
   // a lane's 16 bytes of new row t (rotated); all lanes take part, `here` says whether the row exists
-  auto fetch = [&](int t, bool here) {
-    uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-    if (here) {
-      const T* src;
-      if (SRC == kSrcPages)
-        src = static_cast<const T*>(is_v ? p.v : p.k) + static_cast<int64_t>(phys) * p.src_stride_page + static_cast<int64_t>(kh) * p.src_stride_head + static_cast<int64_t>(t) * p.src_stride_tok + j;
-      else
-        src = static_cast<const T*>(is_v ? p.v : p.k) + static_cast<int64_t>(token_of(t)) * (is_v ? p.v_stride : p.k_stride) + static_cast<int64_t>(kh) * D + j;
-      raw = __ldcs(reinterpret_cast<const uint4*>(src));
-    }
-    return raw;
+  auto source = [&](int t) {
+    if (SRC == kSrcPages)
+      return static_cast<const T*>(is_v ? p.v : p.k) + static_cast<int64_t>(phys) * p.src_stride_page + static_cast<int64_t>(kh) * p.src_stride_head + static_cast<int64_t>(t) * p.src_stride_tok + j;
+    return static_cast<const T*>(is_v ? p.v : p.k) + static_cast<int64_t>(token_of(t)) * (is_v ? p.v_stride : p.k_stride) + static_cast<int64_t>(kh) * D + j;
   };
+  auto fetch = [&](int t, bool here) { return here ? __ldcs(reinterpret_cast<const uint4*>(source(t))) : make_uint4(0u, 0u, 0u, 0u); };
   // the table's part for new row t; on: this lane's elements of it are to be rotated
   auto turn = [&](int t, bool here, bool& on) {
     on = here && j < 2 * p.half;
@@ -260,14 +265,11 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
   auto out_row = [&](int t) { return reinterpret_cast<uint4*>(keep + (static_cast<size_t>(token_of(t)) * p.Hkv + kh) * D + j); };
 
   if constexpr (FMT == kFmtFp8) {
-    // one scale for the page, from its old rows and the new ones together.  A page whose slice a warp can hold (16 pieces per lane) is requested
-    // as a whole and stays in registers; a larger one is gone over twice, for the largest value and for the codes (the second time it
-    // comes from the caches).  That takes 200 registers, one block per SM, and is faster at every size all the same: eight blocks of 32 tokens
-    // 16 us, all twice at two blocks per SM 22.6; 18,000 tokens 164 and 223; 64 single tokens 16.8 and 26.1.
-    constexpr int M = 16;
+    // one scale for the page, from its old rows and the new ones together.  A page that a warp can hold (16 pieces per lane) is requested as
+    // a whole, by asynchronous copies, and stays in shared memory until its codes are written; a larger one is gone over twice.
+    constexpr int M = kApHeld;
     const float old_scale = *page_scale;
     const bool held = p.g <= M * RPI;
-    uint4 all[M];
     auto encode = [&](int t, const uint4& raw, float scale, float inv) {
       float v[8];
       unpack(raw, v);
@@ -288,7 +290,7 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
       for (int x = 0; x < 8; ++x) v[x] *= old_scale;
       return pack(v);                                // exact: four significant bits
     };
-    constexpr int F = 2;                             // rows in flight
+    constexpr int F = fp8_rows(ROLE);                // rows whose part of the table is in flight
     auto values = [&](int tb, uint4 (&raw)[F]) {     // all lanes
 #pragma unroll
       for (int u = 0; u < F; ++u) {
@@ -315,33 +317,42 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
       }
     };
     if (held) {
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < M; ++i) {
         const int t = i * RPI + sub;
-        all[i] = fetch(t, t >= t_lo && t < t_hi);
+        if (t >= t_lo && t < t_hi) copy_async16(hold + 32 * i, source(t));
+        else hold[32 * i] = make_uint4(0u, 0u, 0u, 0u);
       }
-      for (int tb = 0; tb < t_lo; tb += RPI) {       // (few pages have old rows)
-        const int t = tb + sub;
-        const uint2 codes = t < t_lo ? *reinterpret_cast<const uint2*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j) : make_uint2(0u, 0u);
+#pragma unroll 1
+      for (int t = sub; t < t_lo; t += RPI)          // (few pages have old rows)
+        hold[32 * (t / RPI)] = old_row(*reinterpret_cast<const uint2*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j));
+      asm volatile("cp.async.wait_all;" ::: "memory");      // a lane reads what it has copied itself
+#pragma unroll 1
+      for (int tb = 0; tb < t_hi; tb += RPI * F) {
+        uint4 raw[F];
 #pragma unroll
-        for (int i = 0; i < M; ++i)
-          if (i * RPI == tb && t < t_lo) all[i] = old_row(codes);
-      }
+        for (int u = 0; u < F; ++u) raw[u] = hold[32 * (tb / RPI + u)];
+        if (rot && tb + RPI * F > t_lo) {
+          Turn<V> tn[F];
+          bool on[F];
 #pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const int t = i * RPI + sub;
-        if (rot && i * RPI < t_hi && i * RPI + RPI > t_lo) {
-          bool on;
-          const Turn<V> tn = turn(t, t >= t_lo && t < t_hi, on);
-          all[i] = rotate<T, V>(p, all[i], tn, j, on, lane);
+          for (int u = 0; u < F; ++u) tn[u] = turn(tb + u * RPI + sub, tb + u * RPI + sub >= t_lo && tb + u * RPI + sub < t_hi, on[u]);
+#pragma unroll
+          for (int u = 0; u < F; ++u) {
+            raw[u] = rotate<T, V>(p, raw[u], tn[u], j, on[u], lane);
+            hold[32 * (tb / RPI + u)] = raw[u];
+          }
         }
-        if (t < t_hi) {
-          float v[8];
-          unpack(all[i], v);
-          extremes(v);
-        }
+#pragma unroll
+        for (int u = 0; u < F; ++u)
+          if (tb + u * RPI + sub < t_hi) {
+            float v[8];
+            unpack(raw[u], v);
+            extremes(v);
+          }
       }
     } else {
+#pragma unroll 1
       for (int tb = 0; tb < t_hi; tb += RPI * F) {
         uint4 raw[F];
         values(tb, raw);
@@ -361,10 +372,11 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
     const int e = fp8_scale_exp(warp_max(amax));
     const float scale = pow2f(e), inv = pow2f(-e);
     if (held) {
-#pragma unroll
+#pragma unroll 2
       for (int i = 0; i < M; ++i)
-        if (i * RPI + sub < p.g) encode(i * RPI + sub, all[i], scale, inv);
+        if (i * RPI + sub < p.g) encode(i * RPI + sub, hold[32 * i], scale, inv);
     } else {
+#pragma unroll 1
       for (int tb = 0; tb < p.g; tb += RPI * F) {
         uint4 raw[F];
         values(tb, raw);
@@ -498,8 +510,9 @@ __device__ __forceinline__ void rotate_token(const AppendParams& p, int t, int h
 }
 
 template <typename T, int FMT, int D, int SRC, int ROLE>
-__global__ void __launch_bounds__(kApThreads, FMT == kFmtFp8 && SRC == kSrcTokens ? 1 : ROLE == kAll ? 2 : 3) append_kernel(const __grid_constant__ AppendParams p) {
-  extern __shared__ int pre[];                       // [N + 1]
+__global__ void __launch_bounds__(kApThreads, blocks_per_sm(FMT, ROLE)) append_kernel(const __grid_constant__ AppendParams p) {
+  extern __shared__ uint4 shared[];                  // FP8: pages; then [N + 1]
+  int* pre = reinterpret_cast<int*>(reinterpret_cast<char*>(shared) + (FMT == kFmtFp8 ? kApHeldBytes : 0));
   grid_dep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool stored = p.k_pages != nullptr;
@@ -526,7 +539,7 @@ __global__ void __launch_bounds__(kApThreads, FMT == kFmtFp8 && SRC == kSrcToken
       const int item = static_cast<int>(u / (tensors * p.Hkv)), rest = static_cast<int>(u % (tensors * p.Hkv));
       const int s = find_seq(pre, p.N, item);
       const int first_page = SRC == kSrcTokens ? p.start[s] / p.g : 0;
-      append_page<T, FMT, D, SRC, kApRows>(p, s, first_page + item - pre[s], rest % p.Hkv, rest >= p.Hkv, lane);
+      append_page<T, FMT, D, SRC, ROLE>(p, s, first_page + item - pre[s], rest % p.Hkv, rest >= p.Hkv, shared + warp * kApHeld * 32 + lane, lane);
     } else if constexpr (SRC == kSrcTokens && ROLE != kPagesOnly) {
       const long long v = u - page_units;
       const int t = static_cast<int>(v / (q_runs + k_runs)), r = static_cast<int>(v % (q_runs + k_runs));
@@ -541,18 +554,31 @@ template <typename T, int FMT, int D, int SRC, int ROLE>
 int32_t launch_units(losa_ctx* c, const AppendParams& p, long long units, cudaStream_t st) {
   if (units <= 0) return LOSA_OK;
   const long long blocks = std::min<long long>((units + kApWarps - 1) / kApWarps, static_cast<long long>(c->n_sms) * 8);
-  launch_streaming(append_kernel<T, FMT, D, SRC, ROLE>, static_cast<unsigned>(blocks), kApThreads, (p.N + 1) * sizeof(int), st, p);
+  auto kernel = append_kernel<T, FMT, D, SRC, ROLE>;
+  if constexpr (FMT == kFmtFp8) {
+    const size_t bytes = kApHeldBytes + (p.N + 1) * sizeof(int);
+    if (!(c->append_attr_set & (1 << ROLE))) {       // a context has one head dimension and one batch
+      LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+      c->append_attr_set |= 1 << ROLE;
+    }
+    launch_k(kernel, static_cast<unsigned>(blocks), kApThreads, bytes, st, p);
+  } else {
+    launch_streaming(kernel, static_cast<unsigned>(blocks), kApThreads, (p.N + 1) * sizeof(int), st, p);
+  }
   return after_launch(c);
 }
 template <typename T, int FMT, int SRC, int ROLE = kAll>
 int32_t launch_dim(losa_ctx* c, const AppendParams& p, long long units, cudaStream_t st) {
   return c->shape.head_dim == 128 ? launch_units<T, FMT, 128, SRC, ROLE>(c, p, units, st) : launch_units<T, FMT, 64, SRC, ROLE>(c, p, units, st);
 }
-// From so many bytes of queries on, queries and pages are two launches.
-constexpr long long kSplitBytes = 8ll << 20;
+// From so many bytes of queries on, queries and pages are two launches, each with the registers that it needs.  One launch and two, tokens of
+// 32 / 8 heads x 128 (8 KB of queries each): 64 11.2 and 15.2 us, 2,048 16.3 and 24.2, 4,096 31.7 and 37.3, 8,192 58.1 and 57.7, 32,768
+// 240 and 199; into 4 bits 64 15.1 and 19.5, 4,096 36.1 and 42.8, 8,192 66.6 and 68.6, 15,164 119 and 113.
+// FP8, whose pages take most of the time, from a quarter of that on: 1,024 16.9 and 19.3, 2,048 27.1 and 26.4, 4,096 53.7 and 41.5, 8,192 100.6 and 69.4.
+template <int FMT> constexpr long long split_bytes() { return (FMT == kFmtFp8 ? 16ll : 64ll) << 20; }
 template <typename T, int FMT>
 int32_t launch_tokens(losa_ctx* c, const AppendParams& p, long long pages, long long tokens, cudaStream_t st) {
-  if (p.k_pages && p.q_out && tokens * p.Hq * c->shape.head_dim * static_cast<long long>(sizeof(T)) >= kSplitBytes) {
+  if (p.k_pages && p.q_out && tokens * p.Hq * c->shape.head_dim * static_cast<long long>(sizeof(T)) >= split_bytes<FMT>()) {
     const int32_t rc = launch_dim<T, FMT, kSrcTokens, kPagesOnly>(c, p, pages * 2 * p.Hkv, st);
     return rc != LOSA_OK ? rc : launch_dim<T, kFmtNative, kSrcTokens, kQueriesOnly>(c, p, tokens * p.Hq, st);
   }
