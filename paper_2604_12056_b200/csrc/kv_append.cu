@@ -31,8 +31,8 @@ constexpr int kApRows = 2;
 constexpr int kApHeld = 16;
 constexpr int kApHeldBytes = kApWarps * kApHeld * 32 * 16;
 // FP8 pages: two rows' parts of the table in flight and one block per SM in the one launch (few pages: latency), one and two blocks in a launch of
-// its own (many).  64 / 1,024 / 2,048 / 8,192 tokens in one launch: 12.1 / 16.9 / 27.1 / 79.8 us the first way, 16.0 / 17.2 / 22.0 / 69.5 the
-// second; three blocks in a launch of its own: 86.4 instead of 69.4.
+// its own (many).  64 / 1,024 tokens in one launch: 12.1 / 16.9 us the first way, 16.0 / 17.2 the second; 8,192 in two 79.8 and 69.5, with three
+// blocks 86.4.
 constexpr int fp8_rows(int role) { return role == kAll ? 2 : 1; }
 constexpr int blocks_per_sm(int fmt, int role) { return (role == kAll ? 2 : 3) - (fmt == kFmtFp8 ? 1 : 0); }
 constexpr int heads_in_flight(int role) { return role == kAll ? 4 : 8; }
