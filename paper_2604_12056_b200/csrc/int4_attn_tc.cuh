@@ -13,8 +13,8 @@
 //                 passes between the sets before a piece ends.  A row's 64 scores are read once and stay in registers; weights go
 //                 back over them as fp16.  The reference maximum only moves when it would grow by more than 2^8.
 //   O[128 x D] += P V              another issuing warp; A = P from tensor memory, B = values as they lie (tokens x d); 4 instructions per half
-// A block of 32 tokens (128 rows) over eight prompts of 32,768: 183 us, 46 % of the products' own time at the dense bf16 rate; the products and
-// their barriers alone take 132, since an operand in shared memory is read again by every instruction.
+// A block of 32 tokens (128 rows) over eight prompts of 32,768: 183 us (200 over several input sets), where the products need 84 at the dense
+// bf16 rate; they and their barriers alone take 132, since an operand in shared memory is read again by every instruction.
 // Tensor memory is full: two outputs of D columns, two score tiles of 128.  Everything is handed on by mbarriers with bounded waits.
 #pragma once
 
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
         b_scale = scales + ((static_cast<int64_t>(at.x) * p.Hkv + ahead.kh) * GP + (sixteen % SPP) * 16) * RUNS;
         b_valid = at.y;
         // The sixteen groups after these into L2, a row per prefetch: the one group that registers hold in flight covers a hit there, not
-        // memory (eight prompts of 32,768 tokens, a block of 32: 197 -> 183 us).  148 CTAs x 2 tensors x 144 KB lie in the 126 MB.
+        // memory (eight prompts of 32,768 tokens, a block of 32: 198 -> 183 us, over several input sets 207 -> 200).  148 CTAs x 2 tensors x 144 KB lie in the 126 MB.
         const int f = e + 16 * PG;
         if (f < ahead.n_units) {
           const int2 to = i4_resolve(p, ahead, ahead.first_page + f, (sixteen % SPP) * 16, 16);

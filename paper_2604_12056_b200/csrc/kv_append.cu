@@ -108,21 +108,21 @@ __device__ __forceinline__ Turn<V> load_turn(const AppendParams& p, int pos, int
   }
   return t;
 }
-// Two products, two sums, each rounded by itself.
+// two at a time
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 c;
   asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
       : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return c;
 }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 c;
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return c;
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
-// A lane's 16 bytes, rotated.  Products and sums are rounded one by one (no fused multiply-add): the result is that of the formula
-// as it is written, whatever the compiler would contract.  All lanes of the warp take part; `on`: this lane's elements are rotated.
+// A lane's 16 bytes, rotated.  The partner's product is rounded, the element's own is added to it unrounded, said outright so that the result does
+// not hang on what the compiler would contract.  All lanes of the warp take part; `on`: this lane's elements are rotated.
 template <typename T, int V>
 __device__ __forceinline__ uint4 rotate(const AppendParams& p, const uint4& raw, const Turn<V>& t, int j, bool on, int lane) {
   float x[V], y[V];
@@ -130,8 +130,8 @@ __device__ __forceinline__ uint4 rotate(const AppendParams& p, const uint4& raw,
   if (p.interleaved) {
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
-      y[2 * i] = __fsub_rn(__fmul_rn(x[2 * i], t.c[i]), __fmul_rn(x[2 * i + 1], t.s[i]));
-      y[2 * i + 1] = __fadd_rn(__fmul_rn(x[2 * i + 1], t.c[i]), __fmul_rn(x[2 * i], t.s[i]));
+      y[2 * i] = __fmaf_rn(x[2 * i], t.c[i], -__fmul_rn(x[2 * i + 1], t.s[i]));
+      y[2 * i + 1] = __fmaf_rn(x[2 * i + 1], t.c[i], __fmul_rn(x[2 * i], t.s[i]));
     }
   } else {
     const int d = p.half / V, from = on ? (j < p.half ? lane + d : lane - d) : lane;
@@ -144,8 +144,7 @@ __device__ __forceinline__ uint4 rotate(const AppendParams& p, const uint4& raw,
     unpack(o, z);
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
-      const float2 a = mul2(make_float2(x[i], x[i + 1]), make_float2(t.c[i], t.c[i + 1])), b = mul2(make_float2(z[i], z[i + 1]), make_float2(t.s[i], t.s[i + 1]));
-      const float2 r = add2(a, b);
+      const float2 r = fma2(make_float2(x[i], x[i + 1]), make_float2(t.c[i], t.c[i + 1]), mul2(make_float2(z[i], z[i + 1]), make_float2(t.s[i], t.s[i + 1])));
       y[i] = r.x;
       y[i + 1] = r.y;
     }
