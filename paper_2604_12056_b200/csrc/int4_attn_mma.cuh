@@ -1,7 +1,7 @@
 // Attention over 4-bit pages, up to 16 query rows per pass: included by int4_attn.cu (same namespace).
 //
 // What it cannot do without are the cache's bytes (68 per row of 128); what bounds it are the instructions that turn codes into
-// operands: about 640 per unit of 32 tokens, issued at 2.5 a cycle and SM.  Eight prompts of 32,768 tokens, one token each (8 rows per KV
+// operands: about 680 per unit of 32 tokens, issued at 2.1 a cycle and SM.  Eight prompts of 32,768 tokens, one token each (8 rows per KV
 // head): 76 us, 58 % of the copy rate; 16 rows 104; one prompt of 8,192 14.2, most of it latency.  So tokens, not query rows, are the M side of every product, codes become operands in registers, and
 // nothing but codes passes through shared memory:
 //   S^T[16 tokens x 8 rows] += K[16 x 16 d] Q^T[16 d x 8]     mma.sync.m16n8k16, A = keys: a lane takes the quarter
