@@ -365,7 +365,8 @@ int32_t losa_quantize_kv_pages(losa_ctx* ctx, const losa_kv_t* src, losa_kv_t* d
 
 /* Rotation of queries and keys by position, a caller-owned table: row p of cos / sin belongs to position p.
  * Pair j of a head's first rot_dim elements is (x_j, x_{j + rot_dim/2}), or (x_2j, x_{2j+1}) with `interleaved` != 0, and becomes
- *   (x cos - y sin, y cos + x sin)  of its pair (x, y), in fp32 with every product and sum rounded, then rounded once to `dtype`. */
+ *   (x cos - y sin, y cos + x sin)  of its pair (x, y), in fp32 (the product with sin rounded, the one with cos fused into the
+ *   sum), then rounded once to `dtype`. */
 typedef struct {
   const float* cos_table;   /* [n_pos, rot_dim/2] fp32, 16-byte aligned                             */
   const float* sin_table;   /* likewise                                                             */
