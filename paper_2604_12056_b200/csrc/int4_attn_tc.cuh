@@ -288,6 +288,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
         float* record = p.partials + static_cast<size_t>(blockIdx.x + seg) * (R * (D + 2));
         const long long out_row = r < work.rows_of(piece.s) ? i4_row(p, piece.s, piece.kh, r) : -1;
         const float inv = L == 0.f ? 0.f : 4.f / L;
+        __syncwarp();                                    // (the lanes have found their rows each for itself; the loads below need the whole warp)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {               // 16 columns at a time
           const int col = set * (D / 2) + c * 16;

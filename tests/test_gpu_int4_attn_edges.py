@@ -1,0 +1,41 @@
+"""Attention over a 4-bit cache where rows or numbers are out of the ordinary, against the plain 64-bit form (needs a B200)."""
+import pytest
+import torch
+
+import cache_ops_ref as ref
+from test_gpu_int4_attn import Cache
+
+pytestmark = pytest.mark.gpu
+
+# few and many query rows per KV head, by eight, by sixteen, by 128 and with a row group that is not full
+ROWS = [(1, 4), (3, 5), (5, 5), (32, 4), (33, 4)]
+
+
+def dev(*a):
+    return torch.tensor(a, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("g,d", [(32, 64), (32, 128), (16, 128)])
+@pytest.mark.parametrize("block,G", [(5, 5), (9, 5), (31, 3), (33, 4)])
+def test_partly_filled_warps_with_tokens_that_do_not_exist(block, G, g, d):
+    """The lanes of one warp find rows, no rows and rows of tokens outside the block: reported, and the others' results are right,
+    in segments of one CTA and of several."""
+    lens = [40, 9011]
+    c = Cache(lens, block=block, G=G, g=g, d=d, hkv=2, seed=block)
+    B, N, pmax = c.B, 2, c.table.shape[1]
+    act = torch.arange(block, dtype=torch.int32, device="cuda").repeat(N, 1)
+    act[:, 1::4] = block + 7                          # every fourth entry: no such token
+    act[:, 3::8] = -5
+    good = [t for t in range(block) if int(act[0, t]) == t]
+    pages = torch.arange(pmax, dtype=torch.int32, device="cuda").repeat(N, c.hkv, 1).contiguous()
+    count = torch.tensor([[-(-L // g)] * c.hkv for L in lens], dtype=torch.int32, device="cuda")
+    o_p, lse = torch.full(c.q.shape, 55.0, device="cuda"), torch.full_like(c.lse, 55)
+    state = B.make_state(c.q, o_p, lse, c.kv_len)
+    for _ in range(2):
+        B.losa_sparse_prefix_attn(c.ctx, c.q, c.kv, act, dev(block, block), pages, count, state)
+        assert c.ctx.poll_status() == B.LOSA_ERR_BOUNDS
+    off = [t for t in range(block) if t not in good]
+    assert (o_p[:, off] == 55).all() and (lse[:, off] == 55).all()
+    for s in range(N):
+        for h in range(c.hkv):
+            c.check(o_p, lse, s, h, good)
