@@ -556,8 +556,10 @@ int32_t launch_units(losa_ctx* c, const AppendParams& p, long long units, cudaSt
   auto kernel = append_kernel<T, FMT, D, SRC, ROLE>;
   if constexpr (FMT == kFmtFp8) {
     const size_t bytes = kApHeldBytes + (p.N + 1) * sizeof(int);
-    if (!(c->append_attr_set & (1 << ROLE))) {       // a context has one head dimension and one batch
-      LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+    // the most that any context asks for: the limit is the kernel's, whose other contexts have batches of their own
+    constexpr int most = kApHeldBytes + (kMaxSegments + 1) * static_cast<int>(sizeof(int));
+    if (!(c->append_attr_set & (1 << ROLE))) {       // (a context has one head dimension)
+      LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
       c->append_attr_set |= 1 << ROLE;
     }
     launch_k(kernel, static_cast<unsigned>(blocks), kApThreads, bytes, st, p);
