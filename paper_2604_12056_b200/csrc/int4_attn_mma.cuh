@@ -20,6 +20,10 @@
 
 constexpr float kI4Tau = 8.f;                       // log2 units
 constexpr float kI4None = -3e38f;                   // a reference before the first score
+constexpr float kI4MostTau = 1e38f;                 // no threshold is larger: the first score outgrows the reference before it whatever the scale
+// (Scores are fp16 products under 2^36, so none of them meets either of the two.)  A row's factor from scores to log2 units, which is not zero:
+// with rows of zeros and the smallest softmax scales it would be, and -inf times it no number.
+__device__ __forceinline__ float i4_score_scale(int e, float sm_scale) { return fmaxf(__int_as_float((127 - 14 + e) << 23) * (4.f * sm_scale * kLog2e), 1.17549435e-38f); }
 constexpr int i4_warps(int nt) { return nt == 1 ? 12 : 8; }     // most warps of an SM: 168, 255 registers a thread
 
 template <int D> constexpr int i4_unit_codes(int ut) { return ut * D; }          // bytes of a unit's codes, K and V
@@ -191,7 +195,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       // the row's largest element comes to 2^14 .. 2^15
       const int e = max(-100, min(127, static_cast<int>(__float_as_uint(amax) >> 23) - 127));
-      const float up = __int_as_float((127 + 14 - e) << 23), down = __int_as_float((127 - 14 + e) << 23) * (4.f * p.sm_scale * kLog2e);
+      const float up = __int_as_float((127 + 14 - e) << 23), down = i4_score_scale(e, p.sm_scale);
 #pragma unroll
       for (int w = 0; w < WL; ++w) {
         uint32_t h[4];
@@ -217,8 +221,8 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
     for (int nt = 0; nt < NT; ++nt) {
       m[nt][0] = m[nt][1] = kI4None;
       l[nt][0] = l[nt][1] = 0.f;
-      tau[nt][0] = kI4Tau / sc[nt][0];
-      tau[nt][1] = kI4Tau / sc[nt][1];
+      tau[nt][0] = fminf(kI4Tau / sc[nt][0], kI4MostTau);
+      tau[nt][1] = fminf(kI4Tau / sc[nt][1], kI4MostTau);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll

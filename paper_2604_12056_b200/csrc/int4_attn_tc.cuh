@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
       amax = fmaxf(xt[row], xt[R + row]);
       const int e = max(-100, min(127, static_cast<int>(__float_as_uint(amax) >> 23) - 127));       // the largest element comes to 2^14 .. 2^15
       const float up = __int_as_float((127 + 14 - e) << 23);
-      sc = __int_as_float((127 - 14 + e) << 23) * (4.f * p.sm_scale * kLog2e);
+      sc = i4_score_scale(e, p.sm_scale);
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         float v[8];
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
               top2 = max3(top2, score(k + 2), score(k + 3));
             }
             top = fmaxf(top, top2);
-            const bool grow = (top - m) * sc > kI4Tau;
+            const bool grow = (top - m) * sc > kI4Tau || m == kI4None;       // (none yet: whatever the scale)
             if (__any_sync(0xffffffffu, grow)) {
               const float to = grow ? top : m, f = exp2f((m - to) * sc);
               if (used) {                            // the output of all that came before: the half before this one was the last

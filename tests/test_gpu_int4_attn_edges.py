@@ -39,3 +39,28 @@ def test_partly_filled_warps_with_tokens_that_do_not_exist(block, G, g, d):
     for s in range(N):
         for h in range(c.hkv):
             c.check(o_p, lse, s, h, good)
+
+
+def check_rows(c, sm_scale):
+    """All of the cache's rows under another softmax scale."""
+    for s in range(len(c.lens)):
+        for h in range(c.hkv):
+            k, v = c.rows(s, h)
+            heads = slice(h * c.G, (h + 1) * c.G)
+            o, l, do, dl = ref.attention(c.q.cpu()[s, :, heads].double().reshape(-1, c.d), k, v, sm_scale)
+            got, gl = c.out.cpu()[s, :, heads].double().reshape(-1, c.d), c.lse.cpu()[s, :, heads].double().reshape(-1)
+            assert ((got - o).abs() <= do + 2.0 ** -8 * (o.abs() + do)).all()
+            assert ((gl - l).abs() <= dl).all() if k.shape[0] else (gl == -float("inf")).all()
+
+
+@pytest.mark.parametrize("sm_scale", [1e-3, 1e-5, 1e-12, 1e-38, 3.0])
+@pytest.mark.parametrize("block,G", ROWS)
+def test_rows_of_zeros_under_any_softmax_scale(block, G, sm_scale):
+    """Rows of zeros, rows of the smallest bf16 numbers and ordinary ones: the mean of the values and log L, not an empty sum."""
+    c = Cache([130, 1, 0, 9011], block=block, G=G, seed=block)
+    c.q[0] = 0
+    c.q[1::2, :, 0] = 0
+    c.q[3, :, -1] = 2.0 ** -120
+    c.ctx = c.B.Context(4, c.hkv * G, c.hkv, c.d, block, c.g, c.table.shape[1], c.B.LOSA_BF16, sm_scale)
+    assert c.attn() == 0
+    check_rows(c, sm_scale)
