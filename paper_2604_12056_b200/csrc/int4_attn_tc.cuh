@@ -235,11 +235,12 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
               l *= f;
               m = to;
             }
-            const float shift = -m * sc;
+            const float shift = m == kI4None ? 0.f : -m * sc;
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             const float2 scale = make_float2(sc, sc);
-            // a reference so large that only differences can be scaled: subtracted from the scores first
-            const bool apart = __any_sync(0xffffffffu, fabsf(shift) > kTcFused);
+            // a reference so large that only differences can be scaled: subtracted from the scores first (not an infinite one, whose row is
+            // lost: the warp's other rows are computed as they are beside any other)
+            const bool apart = __any_sync(0xffffffffu, fabsf(shift) > kTcFused && fabsf(shift) < INFINITY);
             if (apart) {
 #pragma unroll
               for (int k = 0; k < 64; ++k) x[k] = __float_as_uint(score(k) - m);

@@ -64,3 +64,22 @@ def test_rows_of_zeros_under_any_softmax_scale(block, G, sm_scale):
     c.ctx = c.B.Context(4, c.hkv * G, c.hkv, c.d, block, c.g, c.table.shape[1], c.B.LOSA_BF16, sm_scale)
     assert c.attn() == 0
     check_rows(c, sm_scale)
+
+
+@pytest.mark.parametrize("block,G", ROWS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_no_number_stays_visible(block, G, bad):
+    """One bad element: its row is NaN whether one CTA has the segment or several, the others are as ever."""
+    c = Cache([40, 20011], block=block, G=G, hkv=1, seed=block)
+    c.q[:, 0, 0, 3] = bad
+    c.ks[c.table[:, 0].long(), :, 0] = 100            # (infinity: the first token's key is finite, and not zero there)
+    c.kp[c.table[:, 0].long(), :, 0, 1] = 0x31
+    assert c.attn() == 0
+    assert c.out[:, 0, 0].isnan().all() and c.lse[:, 0, 0].isnan().all()
+    c.q[:, 0, 0, 3] = 0
+    want = c.out.clone(), c.lse.clone()
+    assert c.attn() == 0
+    keep = torch.ones(c.lse.shape, dtype=torch.bool, device="cuda")
+    keep[:, 0, 0] = False
+    assert (c.out[keep] == want[0][keep]).all() and (c.lse[keep] == want[1][keep]).all()
+    c.check_all()
