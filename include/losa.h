@@ -358,7 +358,8 @@ int32_t losa_quantize_kv_pages(losa_ctx* ctx, const losa_kv_t* src, losa_kv_t* d
  * +-7, and stored as code + 8, element 2j of the row in the low half of byte j, element 2j + 1 in the high half.
  * The value every stage works with is scale * code: seven significant bits at most, exact in bf16 and fp16.
  * A row takes d/2 + d/32 bytes, 68 instead of 256 at d = 128.  A token's codes depend on that token alone, so
- * appending leaves the others as they are.  Slots past the prefix's end hold anything and are not read into a result.
+ * appending leaves the others as they are.  A run with a NaN among its elements gets scale byte 255 and is NaN as a
+ * whole wherever it is read (the summaries pass over NaN, as those of the other formats do).  Slots past the prefix's end hold anything and are not read into a result.
  * Stages 2, 3, 5 are unchanged (the summaries are those of the values the codes stand for); stage 4, the whole step,
  * block finalisation, losa_quantize_kv_pages (dst), losa_build_page_summaries and the two calls below take such a
  * cache.  The scale arrays must be 16-byte aligned.  Inputs must satisfy |x| <= 6720 (larger magnitudes saturate). */

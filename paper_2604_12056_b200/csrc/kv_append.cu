@@ -430,9 +430,9 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
         if constexpr (FMT == kFmtInt4) {
           float amax = 0.f;
 #pragma unroll
-          for (int x = 0; x < V; ++x) amax = fmaxf(amax, fabsf(v[x]));
+          for (int x = 0; x < V; ++x) amax = max_nan(amax, fabsf(v[x]));
 #pragma unroll
-          for (int o = 1; o < LRUN; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+          for (int o = 1; o < LRUN; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
           const float scale = int4_scale(amax), mul = int4_multiplier(scale);
           if (amax > 7.f * kInt4MaxScale) {          // saturate
 #pragma unroll
@@ -443,7 +443,7 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
           for (int x = 0; x < V; ++x) {
             const float m = int4_round(v[x], mul);
             w |= int4_bits(m) << (4 * x);
-            v[x] = (m - kInt4Magic) * scale;         // exact
+            v[x] = (m - kInt4Magic) * scale;         // exact; what the pages hold, a NaN too
           }
           if (here) {
             *reinterpret_cast<uint32_t*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j / 2) = w;

@@ -40,11 +40,18 @@ constexpr float kInt4MinScale = 0.000244140625f, kInt4MaxScale = 960.f;
 // Scale of a run: the smallest number of four significant bits >= amax / 7, within the limits.  The quotient
 // is rounded to fp32 first.  amax is a bf16 number: its quotient by 7 either has at most four significant bits, and is exact, or
 // is further than fp32's rounding from any number that has (7 s has seven bits, amax eight).
+// A run with a NaN in it has the scale NaN, and is one in the cache.
 __device__ __forceinline__ float int4_scale(float amax) {
   const uint32_t up = (__float_as_uint(__fdiv_rn(amax, 7.f)) + 0xfffffu) & ~0xfffffu;
-  return fminf(fmaxf(__uint_as_float(up), kInt4MinScale), kInt4MaxScale);
+  return amax != amax ? amax : fminf(fmaxf(__uint_as_float(up), kInt4MinScale), kInt4MaxScale);
 }
-// ... its byte: exponent and mantissa of the fp16 number
+// the larger of two, NaN if one of them is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float c;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+  return c;
+}
+// ... its byte: exponent and mantissa of the fp16 number (NaN: 255)
 __device__ __forceinline__ uint32_t int4_scale_byte(float s) { return __half_as_ushort(__float2half_rn(s)) >> 7; }
 __device__ __forceinline__ float int4_scale_value(uint32_t byte) { return __half2float(__ushort_as_half(static_cast<unsigned short>(byte << 7))); }
 // x / s to the nearest integer, halves away from zero, as the float kInt4Magic + c, whose low four bits are the stored c + 8.

@@ -22,3 +22,64 @@ def test_contexts_of_different_batches_in_turn(kv, dtype, d):
                 t.copy_(old)
         assert c.run() == 0
         c.check()
+
+
+def held(codes, scales):
+    """What 4-bit rows stand for, float64; scale byte 255: NaN."""
+    x = ref.int4_value(ref.int4_unpack(codes.cpu()), scales.cpu().long().clamp(max=247))
+    return torch.where((scales.cpu() == 255).repeat_interleave(32, -1), torch.nan, x)
+
+
+@pytest.mark.parametrize("g,d,rot", [(16, 64, 0), (32, 128, 0), (32, 128, 64), (64, 128, 128)])
+def test_nan_in_4_bit_pages_stays_visible(g, d, rot):
+    """A run with a NaN is NaN in the cache and in k_out / v_out; every other run is as ever; the summaries pass over it."""
+    kw = dict(kv="int4", g=g, d=d, rot=rot, hq=4, hkv=2)
+    a, b = Case([g + 3], [5], **kw), Case([g + 3], [5], **kw)
+    a.k[2, 1, 5] = torch.nan                          # (rotated, it takes its partner along, half the rotated part further on)
+    a.v[g, 0, d - 1] = torch.nan
+    a.v[3, 1, 33] = -torch.nan
+    assert a.run() == 0 and b.run() == 0
+    k_runs = {0} | ({(5 + rot // 2) // 32} if rot else set())
+    bad_k, bad_v = (torch.zeros(g + 3, 2, d // 32, dtype=torch.bool) for _ in range(2))
+    bad_k[2, 1, list(k_runs)] = True
+    bad_v[g, 0, (d - 1) // 32] = bad_v[3, 1, 1] = True
+    at = 5 + torch.arange(g + 3)
+    phys, slot = a.table.cpu()[0].long()[at // g], at % g
+    for bad, pool, scale, other, other_scale, out in ((bad_k, a.kp, a.ks, b.kp, b.ks, a.k_out), (bad_v, a.vp, a.vs, b.vp, b.vs, a.v_out)):
+        codes, bytes_ = pool.cpu()[phys, :, slot], scale.cpu()[phys, :, slot]
+        assert ((bytes_ == 255) == bad).all()
+        same = ~bad
+        assert (codes.unflatten(-1, (-1, 16))[same] == other.cpu()[phys, :, slot].unflatten(-1, (-1, 16))[same]).all()
+        assert (bytes_[same] == other_scale.cpu()[phys, :, slot][same]).all()
+        assert torch.equal(held(codes, bytes_).nan_to_num(nan=1e9), out.cpu().double().nan_to_num(nan=1e9))
+    for page in sorted(set(phys.tolist())):
+        n = g if page == int(a.table[0, 0]) else 8 if g + 8 < 2 * g else g
+        x = held(a.kp[page], a.ks[page])[:, :n]
+        assert (a.kmin[page].cpu().double() == x.nan_to_num(nan=torch.inf).amin(1)).all() and (a.kmax[page].cpu().double() == x.nan_to_num(nan=-torch.inf).amax(1)).all()
+
+
+def test_nan_in_a_bf16_cache_turned_into_4_bits_reaches_the_attention():
+    from paper_2604_12056_b200 import binding as B
+    g, d, hkv, L = 32, 128, 2, 70
+    c = Case([1], [L - 1], kv="native", g=g, d=d, hkv=hkv, hq=8, extra_pages=0)
+    n_phys = c.kp.shape[0]
+    c.kp[c.table[0, 1].long(), 0, 7, 40] = torch.nan   # KV head 0: a key; KV head 1: a value
+    c.vp[c.table[0, 2].long(), 1, 5, 100] = torch.nan
+    c.kp[c.table[0, 2].long(), 1, 6] = torch.nan       # past the end: nothing to see
+    codes = [torch.zeros((n_phys, hkv, g, d // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.full((n_phys, hkv, g, d // 32), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    kv_len = torch.tensor([L], dtype=torch.int32, device="cuda")
+    dst = B.make_kv(*codes, c.kmin, c.kmax, c.table, kv_len, *scales)
+    B.losa_quantize_kv_pages(c.ctx, B.make_kv(c.kp, c.vp, c.kmin, c.kmax, c.table, kv_len), dst)
+    assert c.ctx.poll_status() == 0
+    assert int((scales[0][c.table[0, 1].long()] == 255).sum()) == 1 and int((scales[1][c.table[0, 2].long(), :, :6] == 255).sum()) == 1
+    for block in (1, 3, 32):
+        ctx = B.Context(1, 8, hkv, d, block, g, c.table.shape[1], B.LOSA_BF16, d ** -0.5)
+        q = torch.randn(1, block, 8, d, device="cuda").bfloat16()
+        out, lse = torch.zeros_like(q), torch.zeros(1, block, 8, device="cuda")
+        B.losa_int4_attn(ctx, q, dst, out, lse)
+        assert ctx.poll_status() == 0
+        assert out[:, :, :4].isnan().all() and lse[:, :, :4].isnan().all()
+        bad = torch.zeros(d, dtype=torch.bool, device="cuda")
+        bad[96:] = True
+        assert (out[:, :, 4:].isnan() == bad).all() and lse[:, :, 4:].isfinite().all()
