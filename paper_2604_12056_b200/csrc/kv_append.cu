@@ -386,13 +386,12 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
     __syncwarp();                                    // every lane has read the old scale
     if (lane == 0) *page_scale = scale;
     if (!summaries) return;
-    if (lo[0] <= hi[0]) {                            // encoding is monotone: the extremes of the codes are the codes of the extremes
-      float a[8], b[8];
-      fp8_decode8(fp8_encode8(lo, inv), a);
-      fp8_decode8(fp8_encode8(hi, inv), b);
+    float a[8], b[8];                                // encoding is monotone: the extremes of the codes are the codes of the extremes
+    fp8_decode8(fp8_encode8(lo, inv), a);
+    fp8_decode8(fp8_encode8(hi, inv), b);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) { lo[x] = a[x] * scale; hi[x] = b[x] * scale; }
-    }
+    for (int x = 0; x < 8; ++x)                      // (a column without rows in this lane, or with NaN alone, has none)
+      if (lo[x] <= hi[x]) { lo[x] = a[x] * scale; hi[x] = b[x] * scale; }
   } else {
     uint4 raw[U];                                    // the first rows are requested before those of the page that were there
 #pragma unroll

@@ -83,3 +83,22 @@ def test_nan_in_a_bf16_cache_turned_into_4_bits_reaches_the_attention():
         bad = torch.zeros(d, dtype=torch.bool, device="cuda")
         bad[96:] = True
         assert (out[:, :, 4:].isnan() == bad).all() and lse[:, :, 4:].isfinite().all()
+
+
+@pytest.mark.parametrize("kv,dtype", KINDS)
+@pytest.mark.parametrize("g,d", [(16, 64), (32, 128), (64, 128)])
+def test_summaries_beside_nan_are_those_of_the_cache(kv, dtype, g, d):
+    """NaN in single columns of single tokens, one column with NaN alone: an append leaves the summaries that
+    losa_build_page_summaries makes of the same pages."""
+    c = Case([3, 2 * g, 1], [0, g - 5, g], kv=kv, dtype=dtype, g=g, d=d, rot=0)
+    c.k[1, 0, 0] = c.k[2, 1, 9] = c.k[5, 0, 16] = torch.nan
+    c.k[:3, 0, 8] = torch.nan                         # all tokens of the first page
+    assert c.run() == 0
+    got = c.kmin.clone(), c.kmax.clone()
+    # (rows before the appended ones are part of the cache; pages that no token touched stay as they were)
+    c.B.losa_build_page_summaries(c.ctx, c.kv)
+    assert c.ctx.poll_status() == 0
+    for s, (a, n) in enumerate(zip(c.start, c.new)):
+        for p in range(a // g, (a + n - 1) // g + 1):
+            phys = int(c.table[s, p])
+            assert torch.equal(got[0][phys], c.kmin[phys]) and torch.equal(got[1][phys], c.kmax[phys])
