@@ -362,7 +362,7 @@ int32_t losa_quantize_kv_pages(losa_ctx* ctx, const losa_kv_t* src, losa_kv_t* d
  * whole wherever it is read (the summaries pass over NaN, as those of the other formats do).  Slots past the prefix's end hold anything and are not read into a result.
  * Stages 2, 3, 5 are unchanged (the summaries are those of the values the codes stand for); stage 4, the whole step,
  * block finalisation, losa_quantize_kv_pages (dst), losa_build_page_summaries and the two calls below take such a
- * cache.  The scale arrays must be 16-byte aligned.  Inputs must satisfy |x| <= 6720 (larger magnitudes saturate). */
+ * cache.  The scale arrays, and the rows of a block that is finalised, must be 16-byte aligned (LOSA_ERR_UNSUPPORTED).  Inputs must satisfy |x| <= 6720 (larger magnitudes saturate). */
 
 /* Rotation of queries and keys by position, a caller-owned table: row p of cos / sin belongs to position p.
  * Pair j of a head's first rot_dim elements is (x_j, x_{j + rot_dim/2}), or (x_2j, x_{2j+1}) with `interleaved` != 0, and becomes

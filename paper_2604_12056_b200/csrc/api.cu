@@ -287,6 +287,8 @@ int32_t losa_update_prefix_cache(losa_ctx* ctx, losa_kv_t* kv, losa_state_t* sta
     if (!k_blk || !v_blk) return LOSA_ERR_INVALID_ARG;
     int32_t rc = check_kv(ctx, kv, true);
     if (rc != LOSA_OK) return rc;
+    // (the other formats' kernels take rows of any alignment)
+    if (kv->kv_format == LOSA_KV_INT4 && (!aligned16(k_blk) || !aligned16(v_blk))) return LOSA_ERR_UNSUPPORTED;
   }
   return launch_update_prefix_cache(ctx, kv, state, q, k_blk, v_blk, finalize_block, as_stream(stream));
 }

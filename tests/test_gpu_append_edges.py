@@ -102,3 +102,24 @@ def test_summaries_beside_nan_are_those_of_the_cache(kv, dtype, g, d):
         for p in range(a // g, (a + n - 1) // g + 1):
             phys = int(c.table[s, p])
             assert torch.equal(got[0][phys], c.kmin[phys]) and torch.equal(got[1][phys], c.kmax[phys])
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_block_at_an_odd_address_is_refused_by_4_bit_finalisation(which):
+    c = Case([8, 8], [5, 0], kv="int4", rot=0, packed=False)
+    B = c.B
+    ctx = B.Context(2, c.hq, c.hkv, c.d, 8, c.g, c.table.shape[1], B.LOSA_BF16, 0.1)
+    one = torch.ones(2, dtype=torch.int32, device="cuda")
+    state = B.make_state(c.q_out, c.q_out.float(), one.float(), one)
+    c.kv_len.copy_(c.st)
+    rows = [c.k.data_ptr(), c.v.data_ptr()]
+    rows[which] += 2                                  # (still inside the tensor's first rows; refused before anything is read)
+    launched = ctx.launch_count()
+    with pytest.raises(B.LosaError) as e:
+        B.losa_update_prefix_cache(ctx, c.kv, state, None, *rows, True)
+    assert e.value.code == B.LOSA_ERR_UNSUPPORTED and ctx.launch_count() == launched
+    assert (c.kv_len == c.st).all() and (one == 1).all()
+    B.losa_update_prefix_cache(ctx, c.kv, state, None, c.k, c.v, True)
+    assert ctx.poll_status() == 0
+    c.q_out = c.k_out = None
+    c.check()
