@@ -385,8 +385,8 @@ typedef struct {
   const int32_t* pos_opt;   /* [T] rotation position of every token, or NULL: its position in the sequence */
   int32_t  n_tokens;        /* T                                                                    */
   void*    q_out;           /* [T, H_q, d] rotated queries (may be q, if q is contiguous), or NULL: none wanted  */
-  void*    k_out;           /* [T, H_kv, d] keys as the cache now holds them (dequantised), or NULL  */
-  void*    v_out;           /* [T, H_kv, d] values likewise, or NULL                                 */
+  void*    k_out;           /* [T, H_kv, d] keys as the cache now holds them (dequantised), or NULL; may be k in the same way */
+  void*    v_out;           /* [T, H_kv, d] values likewise, or NULL; may be v                       */
 } losa_new_tokens_t;
 
 /* Appending tokens to the paged cache, rotated on the way.  Token i of sequence s goes to prefix position start[s] + i

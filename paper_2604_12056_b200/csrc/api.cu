@@ -335,6 +335,7 @@ int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, 
   if (!aligned16(tk->q_out) || !aligned16(tk->k_out) || !aligned16(tk->v_out)) return LOSA_ERR_UNSUPPORTED;
   if (tk->q_out && tk->q_out == tk->q && tk->n_tokens > 1 && tk->q_stride != static_cast<int64_t>(sh.n_q_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
   if (tk->k_out && tk->k_out == tk->k && tk->n_tokens > 1 && tk->k_stride != static_cast<int64_t>(sh.n_kv_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
+  if (kv && tk->v_out && tk->v_out == tk->v && tk->n_tokens > 1 && tk->v_stride != static_cast<int64_t>(sh.n_kv_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
   return launch_rope_append(ctx, kv, rope, tk, as_stream(stream));
 }
 

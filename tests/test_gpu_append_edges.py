@@ -123,3 +123,25 @@ def test_a_block_at_an_odd_address_is_refused_by_4_bit_finalisation(which):
     assert ctx.poll_status() == 0
     c.q_out = c.k_out = None
     c.check()
+
+
+@pytest.mark.parametrize("kv,dtype", KINDS)
+def test_outputs_over_their_inputs(kv, dtype):
+    """Contiguous rows may be replaced by what the cache holds of them; rows that lie apart would be overwritten before they are read."""
+    from paper_2604_12056_b200 import binding as B
+    new, start = [70, 1, 200], [3, 64, 31]
+    a, b = (Case(new, start, kv=kv, dtype=dtype, g=64, packed=False) for _ in range(2))
+    assert b.run() == 0
+    B.losa_rope_append(a.ctx, a.kv, a.rope, B.make_new_tokens(a.q, a.k, a.v, a.cu, a.st, None, a.q, a.k, a.v))
+    assert a.ctx.poll_status() == 0
+    for x, y in ((a.q, b.q_out), (a.k, b.k_out), (a.v, b.v_out), (a.kp, b.kp), (a.vp, b.vp)):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+    c = Case(new, start, kv=kv, dtype=dtype)           # rows side by side with the others'
+    launched = c.ctx.launch_count()
+    for name in "qkv":
+        t = B.make_new_tokens(c.q, c.k, c.v, c.cu, c.st, None, c.q_out, c.k_out, c.v_out)
+        setattr(t, name + "_out", getattr(t, name))
+        with pytest.raises(B.LosaError) as e:
+            B.losa_rope_append(c.ctx, c.kv, c.rope, t)
+        assert e.value.code == B.LOSA_ERR_INVALID_ARG
+    assert c.ctx.launch_count() == launched
