@@ -162,7 +162,8 @@ int64_t losa_launch_count(const losa_ctx* ctx);
 
 /* Timing aid.  With `enable` != 0 every later losa_sparse_prefix_attn records a pair of CUDA events
  * (owned by the context) on its stream immediately before and after its main kernel — not around
- * the small combine kernel that follows.  losa_stage4_last_ms waits for the second event and
+ * the small combine kernel that follows (4-bit pages with more than 16 rows per KV head in a block: around two main
+ * kernels and the combine kernel between them).  losa_stage4_last_ms waits for the second event and
  * returns the time between the two in milliseconds (host pointer).  Do not enable while a stream
  * capture is in progress. */
 int32_t losa_profile_stage4(losa_ctx* ctx, int32_t enable);

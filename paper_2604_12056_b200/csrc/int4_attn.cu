@@ -319,6 +319,8 @@ __global__ void __launch_bounds__(kI4CombineWarps * 32) int4_combine_kernel(cons
 
 // ===================================================================== host side
 constexpr int kI4SmemLimit = 232448;
+// Stage 4 is timed from its first main kernel's start to its last one's end (two where the number of rows is known on the device only).
+bool i4_times(const losa_ctx* c, const I4Params& p) { return c->profile && p.n_active; }
 
 template <int D, int NT>
 int mma_smem(int warps, int stages, int ut, int n_sk) {
@@ -343,9 +345,9 @@ int32_t launch_mma(losa_ctx* c, I4Params p, int max_rows, cudaStream_t st) {
   p.pad = many ? 10 : 24;
   int grid = c->n_sms * per_sm;
   grid = std::min<long long>(grid, static_cast<long long>(c->lay.n_slots) * kRowsPerGroup / (2 * R));      // room for the records
-  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
+  if (i4_times(c, p) && p.rows_above == 0) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
   launch_k(kernel, grid, W * 32, mma_smem<D, NT>(W, kI4Ring, UT, p.n_sk), st, p);
-  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
+  if (i4_times(c, p) && p.rows_upto >= p.B * p.G) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
   const int32_t rc = after_launch(c);
   if (rc != LOSA_OK) return rc;
   launch_k(int4_combine_kernel<D, R, false>, (p.n_sk * p.n_rg * R + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);
@@ -366,9 +368,9 @@ int32_t launch_tc(losa_ctx* c, I4Params p, cudaStream_t st) {
   static_assert(tc_smem<D>(kMaxSegments) <= kI4SmemLimit, "shared memory");
   p.n_rg = c->lay.n_row_groups;
   p.pad = 4 * (kTcTok / GP);                         // four groups' time
-  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
+  if (i4_times(c, p) && p.rows_above == 0) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_begin, st));
   launch_k(kernel, c->lay.n_ctas, kTcWarps * 32, tc_smem<D>(p.n_sk), st, p);
-  if (c->profile) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
+  if (i4_times(c, p) && p.rows_upto >= p.B * p.G) LOSA_CUDA_TRY(c, cudaEventRecord(c->ev_end, st));
   const int32_t rc = after_launch(c);
   if (rc != LOSA_OK) return rc;
   launch_k(int4_combine_kernel<D, kTcRows, true>, (p.n_sk * p.n_rg * kTcRows + kI4CombineWarps - 1) / kI4CombineWarps, kI4CombineWarps * 32, 0, st, p);

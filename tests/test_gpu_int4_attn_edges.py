@@ -83,3 +83,26 @@ def test_a_query_that_is_no_number_stays_visible(block, G, bad):
     keep[:, 0, 0] = False
     assert (c.out[keep] == want[0][keep]).all() and (c.lse[keep] == want[1][keep]).all()
     c.check_all()
+
+
+def test_the_time_of_stage_4_is_that_of_the_kernel_that_works():
+    """Eight rows in a context of 128 take what they take in a context of eight (a kernel without work: some 5 us)."""
+    ms = {}
+    for block in (2, 32):
+        c = Cache([32768] * 4, block=block, G=4, hkv=8)
+        B, N, pmax = c.B, 4, c.table.shape[1]
+        act = torch.zeros(N, block, dtype=torch.int32, device="cuda")
+        act[:, 1] = 1
+        pages = torch.arange(pmax, dtype=torch.int32, device="cuda").repeat(N, 8, 1).contiguous()
+        count = torch.full((N, 8), 1024, dtype=torch.int32, device="cuda")
+        state = B.make_state(c.q, torch.zeros(c.q.shape, device="cuda"), torch.zeros_like(c.lse), c.kv_len)
+        c.ctx.profile_stage4(True)
+        ms[block] = []
+        for _ in range(6):
+            B.losa_sparse_prefix_attn(c.ctx, c.q, c.kv, act, dev(*[2] * N), pages, count, state)
+            ms[block].append(c.ctx.stage4_last_ms())
+        assert c.ctx.poll_status() == 0
+        c.attn()                                      # not stage 4: the last one's time stays
+        assert c.ctx.stage4_last_ms() == ms[block][-1]
+    few, many = min(ms[2]), min(ms[32])
+    assert few > 0.02 and 0.8 * few < many < 2 * few + 0.05, ms
