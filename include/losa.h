@@ -407,8 +407,8 @@ int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, 
  * out = sum_t exp(s_t - L) v_t.  With block_size 1 this is a decoding step's attention.  q, out [N, B, H_q, d] (bf16);
  * lse_opt [N, B, H_q] fp32 or NULL.  kv_len[s] = 0 gives out = 0, L = -inf; a longer kv_len than the page-table row holds is
  * cut to it and reported (LOSA_ERR_BOUNDS).  Keys, values and queries are fp16 operands that hold them exactly (a query element below
- * 2^-28 of its row's largest loses low bits), softmax weights are rounded to fp16 (11 significant bits) before
- * their product with the values; sums are fp32.  Another kv_format returns LOSA_ERR_UNSUPPORTED. */
+ * 2^-28 of its row's largest loses low bits), softmax weights are rounded to fp16 before
+ * their product with the values: 11 significant bits down to 2^-21 of the row's largest, below that to within 2^-32 of it; sums are fp32.  Another kv_format returns LOSA_ERR_UNSUPPORTED. */
 int32_t losa_int4_attn(losa_ctx* ctx, const void* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream);
 
 /* Set-up helper — per-page min/max keys of Section 2.3 for the whole prefix: kmin/kmax of every

@@ -19,6 +19,9 @@
 #pragma once
 
 constexpr float kI4Tau = 8.f;                       // log2 units
+// Weights are taken times 2^7, in log2 units: the largest, 2^8 of the reference's, comes to 2^15 and fits fp16, and those below 2^-14 of a row's
+// largest keep their bits: eleven down to 2^-21 of it, and below that to within 2^-32 of it.  A reference that leaves a warp is in the same units.
+constexpr float kI4Lift = 7.f;
 constexpr float kI4None = -3e38f;                   // a reference before the first score
 constexpr float kI4MostTau = 1e38f;                 // no threshold is larger: the first score outgrows the reference before it whatever the scale
 // (Scores are fp16 products under 2^36, so none of them meets either of the two.)  A row's factor from scores to log2 units, which is not zero:
@@ -314,7 +317,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
           for (int b = 0; b < SUBS; ++b) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const float e = ex2((sT[b][nt][c] - m[nt][c & 1]) * sc[nt][c & 1]);
+              const float e = ex2(fmaf(sT[b][nt][c] - m[nt][c & 1], sc[nt][c & 1], kI4Lift));
               sT[b][nt][c] = e;
               l[nt][c & 1] += e;
             }
@@ -390,7 +393,7 @@ int4_mma_kernel(const __grid_constant__ I4Params p) {
         for (int i = 0; i < MT; i += 2)
           *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[nt][i][c], o[nt][i][c + 2], o[nt][i + 1][c], o[nt][i + 1][c + 2]);
         if (gid == 0) {
-          merge_ml[(warp * R + r) * 2] = m[nt][c] == kI4None ? -INFINITY : m[nt][c] * sc[nt][c];
+          merge_ml[(warp * R + r) * 2] = m[nt][c] == kI4None ? -INFINITY : fmaf(m[nt][c], sc[nt][c], -kI4Lift);
           merge_ml[(warp * R + r) * 2 + 1] = l[nt][c];
         }
       }

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + TAIL + 480);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + TAIL + 484);
   int* meta = reinterpret_cast<int*>(gen + TAIL + 512);                  // [kTcMeta][8] valid tokens of every sixteen
-  float* xm = reinterpret_cast<float*>(meta + kTcMeta * 8);              // [set][row] reference maximum (log2 units)
+  float* xm = reinterpret_cast<float*>(meta + kTcMeta * 8);              // [set][row] reference maximum (log2 units, less the weights' lift)
   float* xl = xm + 2 * R;                                                // [set][row] sum of weights
   float* xt = xl + 2 * R;                                                // [half][row] largest element of a query
   int* runs = reinterpret_cast<int*>(xt + 2 * R);
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
               l *= f;
               m = to;
             }
-            const float shift = m == kI4None ? 0.f : -m * sc;
+            const float shift = m == kI4None ? 0.f : fmaf(-m, sc, kI4Lift);
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             const float2 scale = make_float2(sc, sc);
             // a reference so large that only differences can be scaled: subtracted from the scores first (not an infinite one, whose row is
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
 #pragma unroll
               for (int k = 0; k < 64; ++k) x[k] = __float_as_uint(score(k) - m);
             }
-            const float2 sh = apart ? make_float2(0.f, 0.f) : make_float2(shift, shift);
+            const float2 sh = apart ? make_float2(kI4Lift, kI4Lift) : make_float2(shift, shift);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               uint32_t h[16];
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 1) int4_tc_kernel(const __grid_
       // ---- end of the piece: the set's last product, then both sets' outputs, half of the columns each
       const int last = g + groups - 1, mine = ((last & 1) == set ? last : last - 1);
       if (mine >= g) wait(s_free + 8 * (set * 2 + 1), (mine >> 1) & 1);
-      xm[set * R + row] = m == kI4None ? -INFINITY : m * sc;
+      xm[set * R + row] = m == kI4None ? -INFINITY : fmaf(m, sc, -kI4Lift);
       xl[set * R + row] = l;
       tc5_fence_before();
       all_meet();

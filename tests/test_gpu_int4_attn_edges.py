@@ -106,3 +106,35 @@ def test_the_time_of_stage_4_is_that_of_the_kernel_that_works():
         assert c.ctx.stage4_last_ms() == ms[block][-1]
     few, many = min(ms[2]), min(ms[32])
     assert few > 0.02 and 0.8 * few < many < 2 * few + 0.05, ms
+
+
+@pytest.mark.parametrize("block,G", ROWS)
+@pytest.mark.parametrize("down", [16.0, 20.5, 23.0, 26.0])
+def test_small_weights_count(block, G, down):
+    """Every 32nd token takes nearly all weight and has values of zero; what comes out is made of weights 2^-down of its weight.
+    They keep 11 bits down to 2^-21 of the largest and are within 2^-32 of it below."""
+    L, d, hkv = 3001, 128, 2
+    c = Cache([L], block=block, G=G, hkv=hkv, d=d)
+    c.kp[:], c.vp[:] = 0x88, 0xff                     # keys 0, values 7 * scale
+    c.ks[:], c.vs[:] = 120, 100                       # 1 and 2^(12 - 15) * 1.5
+    tall = torch.arange(5, L, 32, device="cuda")
+    page, slot = c.table[0].long()[tall // c.g], tall % c.g
+    for h in range(hkv):
+        c.kp[page, h, slot, 0] = 0x8f                 # element 0: 7
+        c.vp[page, h, slot] = 0x88
+    c.q[:] = 0
+    c.q[..., 0] = down * 0.6931472 * d ** 0.5 / 7     # (rounded to bf16: the reference takes it as it is)
+    assert c.attn() == 0
+    for h in range(hkv):
+        k, v = c.rows(0, h)
+        heads = slice(h * G, (h + 1) * G)
+        q = c.q.cpu()[0, :, heads].double().reshape(-1, d)
+        s = q @ k.T * d ** -0.5
+        p = torch.softmax(s, -1)
+        o, l, _, dl = ref.attention(q, k, v, d ** -0.5)
+        # scores: one product, exact in the accumulator; the factor, the reference, the exponent and the exponential are within 2^-22 of exponents
+        # up to 2^5: 2^-17 of each weight; fp32 sums of 3,001 terms 2^-12 at most
+        do = o.abs() * (2.0 ** -11 + 2.0 ** -16 + 2.0 ** -12) + L * 2.0 ** -32 * p.amax(-1, keepdim=True) * v.abs().amax() + 2.0 ** -8 * o.abs()
+        got = c.out.cpu()[0, :, heads].double().reshape(-1, d)
+        assert ((got - o).abs() <= do).all(), float(((got - o).abs() / do).max())
+        assert ((c.lse.cpu()[0, :, heads].double().reshape(-1) - l).abs() <= dl).all()
