@@ -286,14 +286,18 @@ __global__ void __launch_bounds__(kI4CombineWarps * 32) int4_combine_kernel(cons
     float top = M;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) top = fmaxf(top, m[i]);
-    const float to = top == -INFINITY ? 0.f : top;   // (records without a reference count for nothing, unless their sums are no numbers)
-    const float keep = exp2f(M - to);
+    if (top == -INFINITY) {                          // no record with a reference so far: their sums are zero, or no number, which stays visible
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) L += l[i];
+      continue;
+    }
+    const float keep = exp2f(M - top);
     L *= keep;
 #pragma unroll
     for (int c = 0; c < C; ++c) acc[c] *= keep;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const float f = exp2f(m[i] - to);
+      const float f = exp2f(m[i] - top);
       L = fmaf(l[i], f, L);
 #pragma unroll
       for (int c = 0; c < C; ++c) acc[c] = fmaf(x[i][c], f, acc[c]);
