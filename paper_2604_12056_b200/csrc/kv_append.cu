@@ -427,12 +427,13 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
         float v[V];
         unpack(raw[u], v);
         if constexpr (FMT == kFmtInt4) {
-          float amax = 0.f;
+          float amax = fabsf(v[0]);                  // the run's largest value; a NaN is kept
 #pragma unroll
-          for (int x = 0; x < V; ++x) amax = max_nan(amax, fabsf(v[x]));
+          for (int x = 1; x + 1 < V; x += 2) amax = max_nan(amax, fabsf(v[x]), fabsf(v[x + 1]));
+          amax = max_nan(amax, fabsf(v[V - 1]), 0.f);
 #pragma unroll
-          for (int o = 1; o < LRUN; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-          const float scale = int4_scale(amax), mul = int4_multiplier(scale);
+          for (int o = 1; o < LRUN; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o), 0.f);
+          const float scale = int4_scale(amax), mul = int4_multiplier(scale), held = int4_held_scale(scale, amax);
           if (amax > 7.f * kInt4MaxScale) {          // saturate
 #pragma unroll
             for (int x = 0; x < V; ++x) v[x] = fminf(fmaxf(v[x], -7.f * kInt4MaxScale), 7.f * kInt4MaxScale);
@@ -442,11 +443,11 @@ __device__ __forceinline__ void append_page(const AppendParams& p, int s, int pa
           for (int x = 0; x < V; ++x) {
             const float m = int4_round(v[x], mul);
             w |= int4_bits(m) << (4 * x);
-            v[x] = (m - kInt4Magic) * scale;         // exact; what the pages hold, a NaN too
+            v[x] = (m - kInt4Magic) * held;          // exact; what the pages hold, a NaN too
           }
           if (here) {
             *reinterpret_cast<uint32_t*>(row0 + static_cast<int64_t>(t) * p.stride_tok + j / 2) = w;
-            if ((lane & (LRUN - 1)) == 0) run_scale[t * RUNS + j / kInt4Run] = static_cast<uint8_t>(int4_scale_byte(scale));
+            if ((lane & (LRUN - 1)) == 0) run_scale[t * RUNS + j / kInt4Run] = static_cast<uint8_t>(int4_scale_byte(held));
             if (keep) *out_row(t) = pack(v);
           }
         } else if (here) {

@@ -40,16 +40,17 @@ constexpr float kInt4MinScale = 0.000244140625f, kInt4MaxScale = 960.f;
 // Scale of a run: the smallest number of four significant bits >= amax / 7, within the limits.  The quotient
 // is rounded to fp32 first.  amax is a bf16 number: its quotient by 7 either has at most four significant bits, and is exact, or
 // is further than fp32's rounding from any number that has (7 s has seven bits, amax eight).
-// A run with a NaN in it has the scale NaN, and is one in the cache.
 __device__ __forceinline__ float int4_scale(float amax) {
   const uint32_t up = (__float_as_uint(__fdiv_rn(amax, 7.f)) + 0xfffffu) & ~0xfffffu;
-  return amax != amax ? amax : fminf(fmaxf(__uint_as_float(up), kInt4MinScale), kInt4MaxScale);
+  return fminf(fmaxf(__uint_as_float(up), kInt4MinScale), kInt4MaxScale);
 }
-// the larger of two, NaN if one of them is
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float c;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
-  return c;
+// ... and as the cache holds it: a run with a NaN in it is NaN
+__device__ __forceinline__ float int4_held_scale(float scale, float amax) { return amax != amax ? amax : scale; }
+// the largest of three, NaN if one of them is
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 // ... its byte: exponent and mantissa of the fp16 number (NaN: 255)
 __device__ __forceinline__ uint32_t int4_scale_byte(float s) { return __half_as_ushort(__float2half_rn(s)) >> 7; }
