@@ -242,6 +242,7 @@ attn_tc5_kernel(const __grid_constant__ Tc5Maps<BOTH> maps, AttnParams p) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 0) {                                 // tensor memory: taken while the previous kernel drains
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -903,6 +904,7 @@ attn_tc5_kernel(const __grid_constant__ Tc5Maps<BOTH> maps, AttnParams p) {
           }
           // ---- pass 2: P = 2^(s - m) as 16-bit values, written over the scores (columns 2c, 2c+1 of P take the
           //      place of column c of S, which has been read by then)
+          __syncwarp();                                         // (the lanes' references have moved or not)
           if (ok) {
             const float ms = (m_ref == -INFINITY) ? 0.f : m_ref;
 #pragma unroll 1
@@ -1002,6 +1004,7 @@ attn_tc5_kernel(const __grid_constant__ Tc5Maps<BOTH> maps, AttnParams p) {
             for (int e = 0; e < 32; e += 4)
               *reinterpret_cast<float4*>(rec + 2 * kTileRows + rr * D + c0 + e) = make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
           }
+          __syncwarp();                                         // (the next load of tensor memory needs the whole warp)
         }
         if (h == 0 && r < rows) {
           const float m_last = mref[((g - 1) % kTc5Sets) * kRowsPerGroup + r];

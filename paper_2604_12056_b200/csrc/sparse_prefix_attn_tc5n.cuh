@@ -390,7 +390,10 @@ __device__ __forceinline__ void tc5n_softmax(const AttnParams& p, const Tc5Cta& 
         uint32_t v[8], w[kTc5PTerms][4];                          // (the scores in two halves: all 16 spill registers)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-          if (e % 8 == 0) tc5_ld8(s_at + e, v);
+          if (e % 8 == 0) {
+            if (e > 0) __syncwarp();                            // (lanes without a token have added nothing)
+            tc5_ld8(s_at + e, v);
+          }
           float2 y[2];
           exponents(neg_use, e, v + e % 8, y);
           y[0] = make_float2(ex2(y[0].x), ex2(y[0].y));
@@ -486,6 +489,7 @@ __device__ __forceinline__ void tc5n_softmax(const AttnParams& p, const Tc5Cta& 
       rec[lane % kTileRows] = M;
       rec[kTileRows + lane % kTileRows] = L;
     }
+    __syncwarp();
     const int d = quarter * 32 + lane;
 #pragma unroll 1
     for (int n0 = 8 * h; n0 < rows; n0 += 8 * SB) {       // eight rows at a time, dealt out to the sets
