@@ -145,3 +145,35 @@ def test_outputs_over_their_inputs(kv, dtype):
             B.losa_rope_append(c.ctx, c.kv, c.rope, t)
         assert e.value.code == B.LOSA_ERR_INVALID_ARG
     assert c.ctx.launch_count() == launched
+
+
+@pytest.mark.parametrize("kv,dtype,g,T", [("native", "bf16", 32, 8200), ("native", "f32", 32, 4100), ("int4", "bf16", 16, 8200), ("fp8", "bf16", 64, 2100), ("fp8", "bf16", 32, 2100)])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_prompts_whose_pages_and_queries_are_two_launches(kv, dtype, g, T, pairs):
+    """Just beyond 64 MB of queries (FP8: 16 MB), a ragged batch with starts inside pages, an empty sequence and one of a single token."""
+    new = [T // 2 - 3, 0, 1, T // 4 + 5, 9]
+    new.append(T - sum(new))
+    start = [7, 3, g - 1, 2 * g + 5, 5, 0]
+    c = Case(new, start, kv=kv, dtype=dtype, g=g, hq=32, hkv=2, rot=96, interleaved=pairs, seed=T)
+    launched = c.ctx.launch_count()
+    assert c.run() == 0 and c.ctx.launch_count() == launched + 2
+    c.check()
+
+
+def test_the_larger_launch_below_the_limits_is_one():
+    for kv, T in (("int4", 8190), ("fp8", 2040)):
+        c = Case([T - 50, 50], [9, 40], kv=kv, hq=32, hkv=2, rot=64, g=32, outs=True)
+        launched = c.ctx.launch_count()
+        assert c.run() == 0 and c.ctx.launch_count() == launched + 1
+        c.check()
+
+
+@pytest.mark.parametrize("kv,T", [("native", 8200), ("fp8", 2100)])
+def test_two_launches_leave_alone_what_does_not_fit(kv, T):
+    from paper_2604_12056_b200 import binding as B
+    new, start = [T - 40, 30, 10], [5, 90, 0]
+    c = Case(new, start, kv=kv, hq=32, hkv=2, g=32, n_pos=T - 35)
+    c.st[1] = T                                        # past the rotation table and the row of pages
+    c.start[1] = T
+    assert c.run() == B.LOSA_ERR_BOUNDS
+    c.check(skipped=(1,))
