@@ -64,7 +64,8 @@ __device__ __forceinline__ void i4_finish(const I4Params& p, int s, int kh, int 
 // A word of eight codes becomes four half2 operands with their scale in ten instructions: two shifts, and
 // for each half2 one LOP3 ((x & mask) | 0x6400: 1024 + 4u or 1024 + 64u as fp16) and one HFMA2 whose result,
 // scale * (u - 8) / 4, is exact: scales have four significant bits, so the addends 66 scale and 6 scale have ten and six.
-// (The quarter keeps 66 scale below fp16's end for scales up to 960; the softmax scale and the end result take it back.)
+// (The quarter keeps 66 scale below fp16's end for scales up to 960; the softmax scale and the end result take it back.)  Integers put into the
+// mantissa of 1024 as fp16 are a published way (Kim, Henry, Fahim, Awadalla: Who Says Elephants Can't Run, 2022); two places and one fused step are this format's.
 //
 // (x & MASK) | 0x6400 of both halves, as one instruction
 template <uint32_t MASK>

@@ -1,8 +1,9 @@
 // Attention over 4-bit pages, up to 16 query rows per pass: included by int4_attn.cu (same namespace).
 //
-// What it cannot do without are the cache's bytes (68 per row of 128); what bounds it are the instructions that turn codes into
-// operands: about 680 per unit of 32 tokens, issued at 2.1 a cycle and SM.  Eight prompts of 32,768 tokens, one token each (8 rows per KV
-// head): 76 us, 58 % of the copy rate; 16 rows 104; one prompt of 8,192 14.2, most of it latency.  So tokens, not query rows, are the M side of every product, codes become operands in registers, and
+// What it cannot do without are the cache's bytes (68 per row of 128); what bounds it are instructions and their latencies: about 680 per
+// unit of 32 tokens, half of them conversion and products, issued at 2.1 a cycle and SM of four possible, which is what three warps per scheduler
+// (two at 16 rows, with 255 registers) cover.  Eight prompts of 32,768 tokens, one token each (8 rows per KV
+// head): 75 us, 59 % of the copy rate; 16 rows 104; one prompt of 8,192 14.5, most of it latency.  So tokens, not query rows, are the M side of every product, codes become operands in registers, and
 // nothing but codes passes through shared memory:
 //   S^T[16 tokens x 8 rows] += K[16 x 16 d] Q^T[16 d x 8]     mma.sync.m16n8k16, A = keys: a lane takes the quarter
 //                                (d/4 elements, 16 bytes at d = 128) of two rows that lies in one piece; which elements the

@@ -13,8 +13,9 @@
 //                 passes between the sets before a piece ends.  A row's 64 scores are read once and stay in registers; weights go
 //                 back over them as fp16.  The reference maximum only moves when it would grow by more than 2^8.
 //   O[128 x D] += P V              another issuing warp; A = P from tensor memory, B = values as they lie (tokens x d); 4 instructions per half
-// A block of 32 tokens (128 rows) over eight prompts of 32,768: 183 us (200 over several input sets), where the products need 84 at the dense
-// bf16 rate; they and their barriers alone take 132, since an operand in shared memory is read again by every instruction.
+// A block of 32 tokens (128 rows) over eight prompts of 32,768: 201 us over several input sets (183 with two in turn, as the steps below were
+// timed), where the products need 84 at the dense bf16 rate; they and their barriers alone take 132, since an operand in shared memory is read
+// again by every instruction.
 // Tensor memory is full: two outputs of D columns, two score tiles of 128.  Everything is handed on by mbarriers with bounded waits.
 #pragma once
 

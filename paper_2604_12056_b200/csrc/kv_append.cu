@@ -2,7 +2,8 @@
 // summaries (losa_rope_append); the same pass without rotation appends a finished block to 4-bit pages, turns a bf16
 // cache into 4-bit pages and summarises 4-bit pages.
 //
-// A copy with a little arithmetic on the way, so HBM bounds it (32,768 tokens of 32 / 8 heads x 128, bf16: 184 us, 70 % of the copy rate), and a chain of dependent reads (lengths, page table,
+// A copy with a little arithmetic on the way, so HBM bounds it (32,768 tokens of 32 / 8 heads x 128, bf16: 184 us, 70 % of the copy rate; the
+// queries' launch 83 %, the pages' 52 %: two pieces a lane are too few in flight), and a chain of dependent reads (lengths, page table,
 // rows) when there are few tokens.  Work is cut into units of one warp each, handed out over a flat list, so ragged
 // batches leave no warp idle and empty sequences cost nothing:
 //   (touched page, tensor, KV head)   the new rows of a page: 16 bytes of a row per lane, four loads in flight,
@@ -24,8 +25,8 @@ constexpr int kApWarps = 8, kApThreads = kApWarps * 32;
 constexpr int kFmtNative = 0, kFmtFp8 = 1, kFmtInt4 = 2;
 // what a launch does: all of it, the pages, the queries (two launches, with the registers that each needs, where there is much to do)
 constexpr int kAll = 0, kPagesOnly = 1, kQueriesOnly = 2;
-// ... and the 16-byte pieces that a lane has in flight: of a page's rows (four, with the table's parts beside them, spill at three
-// blocks per SM: 32,768 tokens 226 us, 186 with two), of a token's heads.
+// ... and the 16-byte pieces that a lane has in flight: of a page's rows (at three blocks per SM, 80 registers a thread, four with the table's
+// parts beside them spill 630 to 760 bytes: 32,768 tokens 226 us; two still spill 56 to 80: 186), of a token's heads (eight, 120 bytes).
 constexpr int kApRows = 2;
 // 16-byte pieces per lane of an FP8 page that a warp holds in shared memory
 constexpr int kApHeld = 16;
