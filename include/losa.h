@@ -411,6 +411,61 @@ int32_t losa_rope_append(losa_ctx* ctx, losa_kv_t* kv, const losa_rope_t* rope, 
  * their product with the values: 11 significant bits down to 2^-21 of the row's largest, below that to within 2^-32 of it; sums are fp32.  Another kv_format returns LOSA_ERR_UNSUPPORTED. */
 int32_t losa_int4_attn(losa_ctx* ctx, const void* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream);
 
+/* New tokens of all sequences over the cache, and which of its keys each of them sees.  Sequence s owns tokens cu[s] .. cu[s+1] - 1;
+ * token t of it stands at place p = start[s] + t - cu[s] of the cache, whether it is stored there already or not (a block that is being denoised is not), and
+ * sees key j of the sequence where
+ *     j < kv_len[s],   j < (p / span + 1) * span,   and   window == 0  or  j > p - window  or  j < sinks.
+ * span 1 is causal; with a longer one the tokens of a run of `span` places see one another, as the blocks of a block-wise model do.
+ * Places are those in the cache: after an eviction they count the tokens that are left. */
+#define LOSA_MAX_SPAN 65536
+typedef struct {
+  const void*    q;         /* [T] rows of H_q*d contiguous elements (dtype), 16-byte aligned        */
+  int64_t        q_stride;  /* elements from a token's row to the next; byte stride a multiple of 16 */
+  const int32_t* cu;        /* [N+1] first token of each sequence; cu[N] <= T; sequences may have none */
+  const int32_t* start;     /* [N] place of each sequence's first token                             */
+  int32_t n_tokens;         /* T, at most N * (P_max * g + B)                                       */
+  int32_t max_tokens;       /* the most tokens any sequence has (1: a decoding step)                */
+  int32_t window;           /* keys before (and with) its own place that a token sees; 0: all       */
+  int32_t sinks;            /* first keys that stay visible                                         */
+  int32_t span;             /* >= 1, at most LOSA_MAX_SPAN                                          */
+} losa_queries_t;
+
+/* Attention of new tokens over the paged cache (Section 2.2 with the keys above): s_j = sm_scale * <q, k_j>;
+ * L = log sum_j exp(s_j);  out = sum_j exp(s_j - L) v_j  over the keys that the token sees.  A token that sees none has out = 0, L = -inf.
+ *   out [T, H_q, d] (dtype), not q itself;  lse_opt [T, H_q] fp32 or NULL.  Every kv_format.  out and lse_opt in the layout of a block ([N, B, H_q, d])
+ *   are what losa_block_attn_merge takes as o_p (LOSA_STATE_BF16 in bf16 contexts) and lse_p.
+ *   Rows of tokens that no sequence owns are left as they are.  A sequence with more than max_tokens tokens has the first max_tokens computed, one whose
+ *   kv_len is more than its page-table row holds is cut to that, one whose tokens are not all in 0 .. T - 1, or whose start is negative or
+ *   above 2^30, is left out; each is reported (LOSA_ERR_BOUNDS).  So is a page-table entry outside the pool; what is computed with it is meaningless. */
+int32_t losa_window_attn(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream);
+
+/* The softmax weight that the cached tokens receive from new tokens, added up per KV head:
+ *     weights[j] = (j < start[s] ? keep * weights[j] : 0) + sum over the tokens that see j and the G heads of exp(sm_scale * <q, k_j> - lse)
+ *   for j < kv_len[s] (what stands there for tokens that are new is not read).  lse [T, H_q] fp32: the tokens' log-normalisers, of losa_window_attn
+ *   with the same losa_queries_t, or of a softmax over more keys (losa_block_attn_merge).  A token whose lse is -inf gives nothing.
+ *   weights [n_phys_pages, H_kv, g] fp32, a weight beside every slot of the pool;  keep >= 0 and finite: 1 adds, less forgets.
+ *   Sums are fp32 in an order that is fixed for a call's arguments.  Reports and limits as for losa_window_attn. */
+int32_t losa_kv_weights(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, void* stream);
+
+/* How far sequences are cut down. */
+typedef struct {
+  const int32_t* length;    /* [N] tokens in the cache; not the array kv->kv_len itself             */
+  const int32_t* budget;    /* [N] tokens to keep; a sequence with budget >= length, or a negative one, is left as it is */
+  int32_t* kept;            /* [N, H_kv, kept_stride] out: for each head the former places of the tokens that stay, ascending */
+  int32_t  kept_stride;     /* at least the largest budget below its length                          */
+  int32_t  sinks;           /* first tokens that always stay                                        */
+  int32_t  recent;          /* last tokens that always stay                                         */
+} losa_eviction_t;
+
+/* Eviction by accumulated weight, head by head.  For every sequence with b = budget[s] < L = length[s] and every KV head the first min(sinks, b) tokens, the
+ * last min(recent, b - that) and the b - both of the others with the largest weights stay (equal weights: the lower place;
+ * a NaN is larger than any number).  Their rows move in place to 0 .. b - 1 in order, their weights with them; native and 4-bit rows as they are, FP8 pages 0 .. ceil(b / g) - 1 are
+ * quantised again from their dequantised rows as by block finalisation, their slots behind b hold code 0 then.  kmin / kmax of these pages are recomputed (left out when both are NULL) and
+ * kv_len[s] = b.  Only the first b entries of kept are written.  Places behind b keep what they held (but for FP8's last page); pages behind ceil(b / g) are the
+ * caller's to hand out again.  Pages that a sequence shares with another must not be evicted from.  A sequence whose length is not in 0 .. P_max * g, whose budget is
+ * above kept_stride, or one of whose pages is not of the pool, is left as it is and reported (LOSA_ERR_BOUNDS). */
+int32_t losa_kv_evict(losa_ctx* ctx, losa_kv_t* kv, float* weights, const losa_eviction_t* ev, void* stream);
+
 /* Set-up helper — per-page min/max keys of Section 2.3 for the whole prefix: kmin/kmax of every
  * logical page p < P_s over its valid tokens. */
 int32_t losa_build_page_summaries(losa_ctx* ctx, losa_kv_t* kv, void* stream);

@@ -31,7 +31,7 @@ EXPORTS = [
     "losa_profile_stage4", "losa_stage4_last_ms", "losa_select_active_static",
     "losa_denoise_step", "losa_select_active_tau", "losa_page_scores_topk_pooled",
     "losa_set_pooled_selection", "losa_set_step_selector", "losa_set_wait_limit", "losa_page_scores_topk_mma", "losa_quantize_kv_pages",
-    "losa_rope_append", "losa_int4_attn",
+    "losa_rope_append", "losa_int4_attn", "losa_window_attn", "losa_kv_weights", "losa_kv_evict",
 ]
 
 
@@ -71,6 +71,16 @@ class NewTokensT(C.Structure):
                 ("n_tokens", C.c_int32), ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p)]
 
 
+class QueriesT(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("cu", C.c_void_p), ("start", C.c_void_p), ("n_tokens", C.c_int32),
+                ("max_tokens", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("span", C.c_int32)]
+
+
+class EvictionT(C.Structure):
+    _fields_ = [("length", C.c_void_p), ("budget", C.c_void_p), ("kept", C.c_void_p), ("kept_stride", C.c_int32),
+                ("sinks", C.c_int32), ("recent", C.c_int32)]
+
+
 class StepBuffersT(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("d_q", "d_k_blk", "d_v_blk", "d_out", "active_idx", "n_active",
                                           "topk_pages", "union_pages", "union_count")]
@@ -92,7 +102,7 @@ def lib() -> C.CDLL:
     return _lib
 
 
-# Argument types of the entry points a denoising step calls (p: pointer, i: int32, d: double).  With
+# Argument types of the entry points a denoising step calls (p: pointer, i: int32, f: float, d: double).  With
 # them ctypes converts plain integers itself; without, every argument is wrapped in an object first,
 # and a step of six calls spends more time in that than in its launches.
 _SIGNATURES = {
@@ -102,6 +112,7 @@ _SIGNATURES = {
     "losa_page_union": "ppppippppp", "losa_sparse_prefix_attn": "ppppppppp", "losa_block_attn_merge": "pppppppp",
     "losa_update_prefix_cache": "ppppppip", "losa_quantize_kv_pages": "pppp", "losa_build_page_summaries": "ppp",
     "losa_rope_append": "ppppp", "losa_int4_attn": "pppppp",
+    "losa_window_attn": "pppppp", "losa_kv_weights": "ppppfpp", "losa_kv_evict": "ppppp",
     "losa_denoise_step": "ppppppppppip", "losa_denoise_step_host": "pppppppppip",
 }
 _typed = None
@@ -113,7 +124,7 @@ def _typed_lib() -> C.CDLL:
     if _typed is None:
         lib()                                               # raises when it has not been built
         t = C.CDLL(LIB_PATH)
-        kinds = {"p": C.c_void_p, "i": C.c_int32, "d": C.c_double}
+        kinds = {"p": C.c_void_p, "i": C.c_int32, "d": C.c_double, "f": C.c_float}
         for name, sig in _SIGNATURES.items():
             f = getattr(t, name)
             f.restype, f.argtypes = C.c_int32, [kinds[k] for k in sig]
@@ -193,6 +204,26 @@ def make_new_tokens(q, k, v, cu, start, pos=None, q_out=None, k_out=None, v_out=
     n = NewTokensT(*ptr, *strides, _ptr(cu), _ptr(start), _ptr(pos), T, _ptr(q_out), _ptr(k_out), _ptr(v_out))
     n._keep = (q, k, v, cu, start, pos, q_out, k_out, v_out)
     return n
+
+
+def make_queries(q, cu, start, max_tokens=None, window=0, sinks=0, span=1) -> QueriesT:
+    """losa_queries_t over a [T, H_q, d] tensor whose heads are contiguous within a token's row (the rows may lie anywhere).
+    max_tokens: the most tokens of one sequence (all T where it is not known)."""
+    assert q.is_cuda and q.dim() == 3 and (q.shape[0] == 0 or (q.stride(2) == 1 and (q.shape[1] == 1 or q.stride(1) == q.shape[2])))
+    assert cu.dtype == start.dtype == torch.int32 and cu.numel() == start.numel() + 1
+    T = q.shape[0]
+    x = QueriesT(q.data_ptr(), q.stride(0) if T > 1 else q.shape[1] * q.shape[2], _ptr(cu), _ptr(start), T, T if max_tokens is None else max_tokens,
+                 window, sinks, span)
+    x._keep = (q, cu, start)
+    return x
+
+
+def make_eviction(length, budget, kept, sinks=0, recent=0) -> EvictionT:
+    """losa_eviction_t: length, budget [N] int32, kept [N, H_kv, largest budget] int32."""
+    assert length.dtype == budget.dtype == kept.dtype == torch.int32 and kept.dim() == 3 and length.shape == budget.shape == kept.shape[:1]
+    e = EvictionT(_ptr(length), _ptr(budget), _ptr(kept), kept.shape[2], sinks, recent)
+    e._keep = (length, budget, kept)
+    return e
 
 
 LOSA_STATE_F32, LOSA_STATE_BF16 = 0, 1
@@ -350,6 +381,21 @@ def losa_rope_append(ctx, kv, rope, tokens):
 def losa_int4_attn(ctx, q, kv, out, lse_opt=None):
     """Attention of all block tokens over the whole of a 4-bit cache."""
     ctx._check("losa_int4_attn", _typed_lib().losa_int4_attn(ctx._h, _ptr(q), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
+
+
+def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
+    """Attention of new tokens over the cache, each over the keys it sees (a window and first tokens that stay visible)."""
+    ctx._check("losa_window_attn", _typed_lib().losa_window_attn(ctx._h, C.byref(queries), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
+
+
+def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
+    """The softmax weight that cached tokens receive from new ones, added to keep * weights ([n_phys, H_kv, g] fp32)."""
+    ctx._check("losa_kv_weights", _typed_lib().losa_kv_weights(ctx._h, C.byref(queries), C.byref(kv), _ptr(lse), keep, _ptr(weights), _stream()))
+
+
+def losa_kv_evict(ctx, kv, weights, eviction):
+    """Sequences cut down to their budgets: per KV head the tokens of least weight leave, the others move to the front."""
+    ctx._check("losa_kv_evict", _typed_lib().losa_kv_evict(ctx._h, C.byref(kv), _ptr(weights), C.byref(eviction), _stream()))
 
 
 def losa_build_page_summaries(ctx, kv):

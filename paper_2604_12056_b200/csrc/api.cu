@@ -1,5 +1,6 @@
 // C-ABI layer of the LoSA library: argument validation, context and workspace bookkeeping.
 // Every entry point validates on the host and launches nothing when validation fails.
+#include <algorithm>
 #include <cstdlib>
 #include <cstring>
 #include <new>
@@ -26,6 +27,9 @@ int32_t check_shape(const losa_shape_t* sh) {
   return LOSA_OK;
 }
 
+// New tokens of a sequence that a call of the windowed attention may bring: as many as its pages hold, or a block behind them.
+int64_t max_new_tokens(const losa_shape_t* sh) { return static_cast<int64_t>(sh->max_pages_per_seq) * sh->page_size + sh->block_size; }
+
 int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   const int G = sh->n_q_heads / sh->n_kv_heads;
   L->n_row_groups = (sh->block_size * G + kRowsPerGroup - 1) / kRowsPerGroup;
@@ -42,8 +46,11 @@ int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   L->union_bits = off;
   off = align_up(off + sizeof(uint32_t) * static_cast<size_t>(sh->batch) * sh->n_kv_heads * ((sh->max_pages_per_seq + 31) / 32), 256);
   L->union_tickets = off; off = align_up(off + sizeof(uint32_t) * sh->batch * sh->n_kv_heads, 256);
+  L->evict_ticket = off; off = align_up(off + sizeof(uint32_t), 256);
   L->delta = off;    off = align_up(off + sizeof(double) * sh->batch * sh->block_size, 256);
   L->int4_records = off; off = align_up(off + 2 * sizeof(int32_t) * 16 * L->n_segments, 256);
+  L->plan_tiles = static_cast<int64_t>(sh->batch) * ((max_new_tokens(sh) * G + kPlanRows - 1) / kPlanRows + 1);
+  L->plan = off;     off = align_up(off + 256 + 16 * (static_cast<size_t>(sh->batch) + kPlanShares * n_ctas + 1 + L->plan_tiles), 256);
   L->scores = off;
   off = align_up(off + 2 * sizeof(float) * static_cast<size_t>(sh->batch) * sh->block_size * sh->n_q_heads * L->score_stride, 256);
   L->partials = off;
@@ -51,7 +58,7 @@ int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   const size_t rows = static_cast<size_t>(sh->batch) * sh->block_size * sh->n_q_heads;
   L->block_o = off;   off = align_up(off + sizeof(float) * rows * sh->head_dim, 256);
   L->block_lse = off; off = align_up(off + sizeof(float) * rows, 256);
-  L->total = off;
+  L->total = std::max(off, align_up(L->scores + sizeof(float) * static_cast<size_t>(n_ctas) * kPlanRecordRows * (sh->head_dim + 2), 256));
   return LOSA_OK;
 }
 
@@ -90,6 +97,18 @@ int32_t check_kv(const losa_ctx* c, const losa_kv_t* kv, bool need_summaries) {
       (kv->kmax && !aligned16(kv->kmax)))
     return LOSA_ERR_UNSUPPORTED;
   return LOSA_OK;
+}
+
+// The tokens of a call over the cache.
+int32_t check_queries(const losa_ctx* c, const losa_queries_t* q) {
+  if (!q || !q->cu || !q->start || q->n_tokens < 0 || q->window < 0 || q->sinks < 0 || q->span < 1 || q->span > LOSA_MAX_SPAN) return LOSA_ERR_INVALID_ARG;
+  const losa_shape_t& sh = c->shape;
+  if (q->n_tokens > (1 << 30) || q->n_tokens > sh.batch * max_new_tokens(&sh)) return LOSA_ERR_UNSUPPORTED;
+  if (q->n_tokens == 0) return LOSA_OK;              // (no rows: their pointer may be null)
+  if (!q->q || q->max_tokens < 1) return LOSA_ERR_INVALID_ARG;
+  if (q->n_tokens > 1 && q->q_stride < static_cast<int64_t>(sh.n_q_heads) * sh.head_dim) return LOSA_ERR_INVALID_ARG;
+  const int64_t es = sh.dtype == LOSA_BF16 ? 2 : 4;
+  return aligned16(q->q) && (q->n_tokens == 1 || q->q_stride * es % 16 == 0) ? LOSA_OK : LOSA_ERR_UNSUPPORTED;
 }
 
 cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
@@ -345,6 +364,35 @@ int32_t losa_int4_attn(losa_ctx* ctx, const void* q, const losa_kv_t* kv, void* 
   if (rc != LOSA_OK) return rc;
   if (kv->kv_format != LOSA_KV_INT4 || !aligned16(q) || !aligned16(out)) return LOSA_ERR_UNSUPPORTED;
   return launch_int4_attn(ctx, q, kv, out, lse_opt, as_stream(stream));
+}
+
+int32_t losa_window_attn(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, void* out, float* lse_opt, void* stream) {
+  if (!ctx) return LOSA_ERR_INVALID_ARG;
+  int32_t rc = check_queries(ctx, q);
+  if (rc == LOSA_OK) rc = check_kv(ctx, kv, false);
+  if (rc != LOSA_OK) return rc;
+  if (q->n_tokens == 0) return LOSA_OK;
+  if (!out || out == q->q) return LOSA_ERR_INVALID_ARG;
+  if (!aligned16(out)) return LOSA_ERR_UNSUPPORTED;
+  return launch_window_attn(ctx, q, kv, out, lse_opt, as_stream(stream));
+}
+
+int32_t losa_kv_weights(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, void* stream) {
+  if (!ctx || !weights || !(keep >= 0.f) || keep > 3.4e38f) return LOSA_ERR_INVALID_ARG;
+  int32_t rc = check_queries(ctx, q);
+  if (rc == LOSA_OK) rc = check_kv(ctx, kv, false);
+  if (rc != LOSA_OK) return rc;
+  if (q->n_tokens > 0 && !lse) return LOSA_ERR_INVALID_ARG;
+  return launch_kv_weights(ctx, q, kv, lse, keep, weights, as_stream(stream));
+}
+
+int32_t losa_kv_evict(losa_ctx* ctx, losa_kv_t* kv, float* weights, const losa_eviction_t* ev, void* stream) {
+  if (!ctx || !weights || !ev || !ev->length || !ev->budget || !ev->kept || ev->kept_stride < 1 || ev->sinks < 0 || ev->recent < 0)
+    return LOSA_ERR_INVALID_ARG;
+  const int32_t rc = check_kv(ctx, kv, false);
+  if (rc != LOSA_OK) return rc;
+  if (!kv->kmin != !kv->kmax || ev->length == kv->kv_len) return LOSA_ERR_INVALID_ARG;
+  return launch_kv_evict(ctx, kv, weights, ev, as_stream(stream));
 }
 
 int32_t losa_build_page_summaries(losa_ctx* ctx, losa_kv_t* kv, void* stream) {

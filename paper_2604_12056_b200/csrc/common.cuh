@@ -25,8 +25,10 @@ struct WorkspaceLayout {
   size_t union_bits;    // uint32[N*H_kv*ceil(P_max/32)] : page bitmaps of the selection.  bf16: the selection writes the union from them, all zero between launches; fp32: stage 4 does, and stage 1 of the next whole step clears them
   size_t union_tickets; // uint32[N*H_kv] : its arrival counters (self-resetting)
   size_t int4_records;  // int2[16 * n_segments] : likewise for the 4-bit attention, whose row groups are smaller
+  size_t evict_ticket;  // uint32 : order of the page-moving kernel's blocks (self-resetting)
   size_t delta;      // double[N*B]
-  size_t scores;     // float[2*N*B*H_q*score_stride]: page scores, or (lower, upper) bound pairs of them
+  size_t plan;       // list of work of the windowed attention: header, sequences, shares, tiles
+  size_t scores;     // float[2*N*B*H_q*score_stride]: page scores, or (lower, upper) bound pairs of them; from here on also what calls of their own keep for their own time (records of the windowed attention, flags of the eviction)
   size_t partials;   // float[n_slots * kRowsPerGroup * (d + 2)]
   size_t block_o;    // float[N*B*H_q*d]  : in-block attention output of the whole-step path
   size_t block_lse;  // float[N*B*H_q]    : its log-normaliser
@@ -36,6 +38,7 @@ struct WorkspaceLayout {
   int32_t n_ctas;        // CTAs of the split-KV attention kernels (one per SM)
   int32_t n_row_groups;  // ceil(B*G / kRowsPerGroup)
   int32_t n_segments;    // N * H_kv * n_row_groups
+  int64_t plan_tiles;    // tiles the plan has room for
 };
 
 }  // namespace losa
@@ -75,6 +78,7 @@ struct losa_ctx {
   int32_t refine_attr_set;
   int32_t int4_attr_set;     // and for the 4-bit attention kernels, a bit each
   int32_t append_attr_set;   // and for the FP8 append kernel, by role
+  int32_t window_attr_set;   // and for the kernels of windowed attention, weights and eviction, a bit each
   // optional timing of the stage-4 main kernel
   int32_t profile;
   cudaEvent_t ev_begin, ev_end;

@@ -110,6 +110,14 @@ int32_t launch_int4_attn(losa_ctx* c, const void* q, const losa_kv_t* kv, void* 
 int32_t launch_int4_prefix_attn(losa_ctx* c, const void* q, const losa_kv_t* kv, const int32_t* active_idx, const int32_t* n_active,
                                 const int32_t* union_pages, const int32_t* union_count, losa_state_t* state, cudaStream_t st);
 
+// New tokens over the cache, each over the keys it sees; what every key gets of them; the tokens of least weight leave.
+// The attention's list of work lies in the workspace: its rows per tile are kPlanRows at least, its CTAs at most kPlanShares per SM, and
+// they leave records of at most kPlanRecordRows rows per SM.
+constexpr int kPlanRows = 64, kPlanShares = 4, kPlanRecordRows = 512;
+int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t* kv, void* out, float* lse_opt, cudaStream_t st);
+int32_t launch_kv_weights(losa_ctx* c, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, cudaStream_t st);
+int32_t launch_kv_evict(losa_ctx* c, losa_kv_t* kv, float* weights, const losa_eviction_t* ev, cudaStream_t st);
+
 // Largest k and page count the top-k kernel's shared memory allows for this context.
 int32_t topk_max_sortable(const losa_ctx* c);
 
