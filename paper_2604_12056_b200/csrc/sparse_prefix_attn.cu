@@ -551,6 +551,8 @@ int32_t launch_f32(losa_ctx* c, const AttnParams& ap, cudaStream_t st, bool with
 }  // namespace
 
 
+int32_t pool_tensor_maps(losa_ctx* c, const losa_kv_t* kv) { return ensure_tensor_maps(c, kv); }
+
 int32_t prepare_sparse_prefix_attn(losa_ctx* c, const losa_kv_t* kv) {
   const bool bf = c->shape.dtype == LOSA_BF16, fp8 = kv->kv_format == LOSA_KV_FP8_E4M3;     // (FP8 pages: bf16 contexts only)
   const int32_t rc = bf ? ensure_tensor_maps(c, kv) : LOSA_OK;

@@ -4,11 +4,15 @@
 // (tile, KV head, group) form one list, cut into equal shares, one per CTA, so prompts, blocks and single tokens of any lengths fill
 // the GPU alike.  A tile that several CTAs share leaves records (reference, sum, un-normalised output per row) that a kernel of
 // its own merges by log-sum-exp.  A first small kernel writes the list's tiles and where each share begins.
+#include <cuda.h>
+
 #include <algorithm>
+#include <cstring>
 #include <type_traits>
 
 #include "cache_view.cuh"
 #include "kernels.h"
+#include "tcgen05_ops.cuh"
 
 namespace losa {
 namespace {
@@ -284,6 +288,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __
 }
 
 #include "window_attn_f32.cuh"
+#include "window_attn_tc.cuh"
 
 // ===================================================================== host side
 template <int R, int GT, int D, typename Launch, typename T>
@@ -317,6 +322,32 @@ int32_t launch_rows(losa_ctx* c, WindowParams& p, cudaStream_t st) {
   });
 }
 
+template <int D, int GP>
+int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_t st) {
+  const int32_t rc = pool_tensor_maps(c, kv);
+  if (rc != LOSA_OK) return rc;
+  CUtensorMap mk, mv;
+  memcpy(&mk, c->tmap_k, sizeof(mk));
+  memcpy(&mv, c->tmap_v, sizeof(mv));
+  p.n_ctas = c->n_sms;
+  p.pad = 2;
+  p.least = 3;
+  auto kernel = window_tc_kernel<D, GP>;
+  if (!(c->window_attr_set & 1)) {
+    static_assert(wt_smem<D>() <= 232448, "shared memory");
+    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wt_smem<D>()));
+    // the kernel moves registers between its warps: a build that is launched with fewer than it deals out would wait for ever
+    cudaFuncAttributes fa;
+    LOSA_CUDA_TRY(c, cudaFuncGetAttributes(&fa, kernel));
+    if (fa.numRegs < kWtLaunchRegs) return LOSA_ERR_UNSUPPORTED;
+    c->window_attr_set |= 1;
+  }
+  return with_plan<kWtRows, kWtKeys, D>(c, p, st, __nv_bfloat16{}, [&]() -> int32_t {
+    launch_k(kernel, p.n_ctas, kWtWarps * 32, wt_smem<D>(), st, mk, mv, p);
+    return after_launch(c);
+  });
+}
+
 }  // namespace
 
 int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t* kv, void* out, float* lse_opt, cudaStream_t st) {
@@ -335,7 +366,13 @@ int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t
   };
   switch (row_format(c, kv)) {
     case kRowsF32: return run(std::integral_constant<int, kRowsF32>{});
-    case kRowsBf16: return run(std::integral_constant<int, kRowsBf16>{});
+    case kRowsBf16: {
+      auto with_page = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        return c->shape.page_size == 16 ? launch_tc<D, 16>(c, p, kv, st) : c->shape.page_size == 32 ? launch_tc<D, 32>(c, p, kv, st) : launch_tc<D, 64>(c, p, kv, st);
+      };
+      return c->shape.head_dim == 128 ? with_page(std::integral_constant<int, 128>{}) : with_page(std::integral_constant<int, 64>{});
+    }
     case kRowsFp8: return run(std::integral_constant<int, kRowsFp8>{});
     default: return run(std::integral_constant<int, kRowsInt4>{});
   }

@@ -102,6 +102,24 @@ def test_queries_of_all_sizes(fmt, amp):
     c.check()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_scores_so_large_that_one_key_takes_all(fmt):
+    c = Cache([300, 77], fmt=fmt, hkv=1, G=1)
+    c.tokens([40, 1], [260, 76])
+    c.q.mul_(1e26 if fmt == "f32" else 1e30)
+    assert c.attend(200, 4, 1) == 0
+    k, v = c.rows("k"), c.rows("v")
+    for s, tokens, ok in c.each():
+        sc = c.q[tokens, 0].cpu().double() @ k[s][:, 0].T
+        sc[~ok] = -float("inf")
+        two = sc.topk(2).values
+        clear = two[:, 0] - two[:, 1] > 1e-5 * two[:, 0].abs()           # (far above what fp32 sums may be off by)
+        want = v[s][:, 0][sc.argmax(-1)]
+        got = c.out[tokens, 0].cpu().double()
+        assert clear.any() and got.isfinite().all()
+        assert ((got - want).abs() <= 2.0 ** -8 * want.abs())[clear].all()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 def test_what_is_no_number_stays_where_it_is_seen(fmt, value):
