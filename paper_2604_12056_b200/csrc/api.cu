@@ -50,7 +50,7 @@ int32_t make_layout(const losa_shape_t* sh, int n_ctas, WorkspaceLayout* L) {
   L->delta = off;    off = align_up(off + sizeof(double) * sh->batch * sh->block_size, 256);
   L->int4_records = off; off = align_up(off + 2 * sizeof(int32_t) * 16 * L->n_segments, 256);
   L->plan_tiles = static_cast<int64_t>(sh->batch) * ((max_new_tokens(sh) * G + kPlanRows - 1) / kPlanRows + 1);
-  L->plan = off;     off = align_up(off + 256 + 16 * (static_cast<size_t>(sh->batch) + kPlanShares * n_ctas + 1 + L->plan_tiles), 256);
+  L->plan = off;     off = align_up(off + 256 + 48 * (static_cast<size_t>(kPlanShares) * n_ctas + 1) + 32 * L->plan_tiles, 256);
   L->scores = off;
   off = align_up(off + 2 * sizeof(float) * static_cast<size_t>(sh->batch) * sh->block_size * sh->n_q_heads * L->score_stride, 256);
   L->partials = off;

@@ -27,7 +27,7 @@ struct QueryParams {
   int T, max_tokens, window, sinks, span;
 };
 // A sequence as it is worked on: its tokens are cu .. cu + count - 1 at places start .., over len keys.
-struct Sequence { int cu, count, start, len; };
+struct alignas(16) Sequence { int cu, count, start, len; };
 
 // What of a sequence can be used (called by one lane per sequence where a report shall come once).
 __device__ __forceinline__ Sequence sequence_of(const CacheParams& c, const QueryParams& q, int s, int32_t* status) {

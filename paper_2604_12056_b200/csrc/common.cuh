@@ -27,7 +27,7 @@ struct WorkspaceLayout {
   size_t int4_records;  // int2[16 * n_segments] : likewise for the 4-bit attention, whose row groups are smaller
   size_t evict_ticket;  // uint32 : order of the page-moving kernel's blocks (self-resetting)
   size_t delta;      // double[N*B]
-  size_t plan;       // list of work of the windowed attention: header, sequences, shares, tiles
+  size_t plan;       // list of work of the windowed attention: header, shares, tiles; and the keys' weights
   size_t scores;     // float[2*N*B*H_q*score_stride]: page scores, or (lower, upper) bound pairs of them; from here on also what calls of their own keep for their own time (records of the windowed attention, flags of the eviction)
   size_t partials;   // float[n_slots * kRowsPerGroup * (d + 2)]
   size_t block_o;    // float[N*B*H_q*d]  : in-block attention output of the whole-step path

@@ -1,0 +1,293 @@
+// The keys' weights on the 5th-generation tensor cores: included by kv_weights.cu (same namespace).
+//
+// Keys take the 128 lanes, query rows the columns, so that a thread has a key to itself and its sum never leaves the register: a job is
+// 128 keys by up to 128 rows.
+//   a warp            pages of keys by TMA into a ring of swizzled tiles
+//   three warps       rows of Q, and their log-normalisers, into another
+//   S[128 x rows] = K Q^T   an issuing warp; four score tiles in tensor memory
+//   two sets of four warps  take alternate jobs: exponentials, added up by key; at a tile's end the sets' sums meet in shared memory
+// A key is seen by a run of rows, so a job that is not seen whole is masked by two numbers per thread.
+#pragma once
+
+constexpr int kKwKeys = 128, kKwRows = 128, kKwBufs = 4, kKwNK = 3, kKwNQ = 3;
+constexpr int kKwSumWarps = 8, kKwLoadWarp = 8, kKwMmaWarp = 9, kKwQWarp = 10, kKwQWarps = 6, kKwWarps = 16;
+template <int D> constexpr int kw_tile() { return 128 * D * 2; }
+template <int D> constexpr int kw_smem() { return 1024 + (kKwNK + kKwNQ) * kw_tile<D>() + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4 + 256; }
+
+// Tiles of keys that have anything to do: those under the first tokens, and from the window of the first token on; all where weights are forgotten.
+struct KeyReach { int first, from, tiles; };
+__device__ __forceinline__ KeyReach key_reach(const ListParams& p, const Sequence& x) {
+  KeyReach r = {0, 0, 0};
+  const int all = (x.len + kKwKeys - 1) / kKwKeys;
+  if (p.keep != 1.f) {
+    r.tiles = all;
+    return r;
+  }
+  const int lo = min(x.start, x.count > 0 ? keys_of(p.q, x, x.start).y : x.start), sinks = lo > 0 && x.count > 0 ? min(p.q.sinks, x.len) : 0;
+  r.first = (sinks + kKwKeys - 1) / kKwKeys;
+  r.from = max(r.first, lo / kKwKeys);
+  r.tiles = r.first + max(0, all - r.from);
+  return r;
+}
+__device__ __forceinline__ int tile_key(const KeyReach& r, int j) { return (j < r.first ? j : r.from + j - r.first) * kKwKeys; }
+struct KeyTiles {
+  static __device__ __forceinline__ int tiles(const ListParams& p, const Sequence& x) { return key_reach(p, x).tiles; }
+  static __device__ __forceinline__ int groups(const ListParams& p, const Sequence& x, int j) {
+    const int key0 = tile_key(key_reach(p, x), j);
+    const int2 rows = rows_over(p, x, key0, min(kKwKeys, x.len - key0));
+    return (rows.y - rows.x + kKwRows - 1) / kKwRows;
+  }
+};
+struct KeyPiece : Part { int key0, row0, rows; };    // rows row0 .. row0 + rows - 1 see any of the tile's keys
+__device__ __forceinline__ KeyPiece next_keys(Walk& walk) {
+  KeyPiece w;
+  static_cast<Part&>(w) = walk.next();
+  if (w.any) {
+    w.key0 = tile_key(key_reach(walk.p, w.x), w.j);
+    const int2 rows = rows_over(walk.p, w.x, w.key0, min(kKwKeys, w.x.len - w.key0));
+    w.row0 = rows.x;
+    w.rows = rows.y - rows.x;
+  }
+  return w;
+}
+
+template <int D, int GP>
+__global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeightParams p) {
+  constexpr int TILE = kw_tile<D>(), HS = 128 * 128, PG = kKwKeys / GP;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw);
+  const uint32_t kring = base, qring = kring + kKwNK * TILE;
+  constexpr int TAIL = (kKwNK + kKwNQ) * TILE;
+  float* norms = reinterpret_cast<float*>(gen + TAIL);                   // [slot][row] log-normaliser in log2 units
+  float* other = norms + kKwNQ * kKwRows;                                // [2][key] the second set's sums, by turns
+  const uint32_t bars = base + TAIL + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4;
+  const uint32_t k_full = bars, k_free = k_full + 8 * kKwNK, q_full = k_free + 8 * kKwNK, q_free = q_full + 8 * kKwNQ;
+  const uint32_t s_full = q_free + 8 * kKwNQ, s_free = s_full + 8 * kKwBufs, drain = s_free + 8 * kKwBufs;
+  constexpr int MISC = TAIL + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4 + 8 * (2 * kKwNK + 2 * kKwNQ + 2 * kKwBufs + 1);
+  static_assert(MISC + 8 - TAIL - kKwNQ * kKwRows * 4 - 2 * kKwKeys * 4 <= 256, "barriers");
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + MISC);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + MISC + 4);
+  const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
+
+  grid_dep_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < kKwNK; ++i) { mbar_init(k_full + 8 * i, 1); mbar_init(k_free + 8 * i, 1); }
+    for (int i = 0; i < kKwNQ; ++i) { mbar_init(q_full + 8 * i, kKwQWarps); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
+    for (int i = 0; i < kKwBufs; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_free + 8 * i, 4); }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  grid_dep_wait();
+  if (static_cast<int>(blockIdx.x) >= p.plan.head[0]) return;            // (one answer for the CTA)
+  __syncwarp();
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc5_fence_before();
+  __syncthreads();
+  tc5_fence_after();
+  const uint32_t tmem = warp_uniform(*tmem_slot);
+  // a bound shorter than a look at a barrier takes has run out by then (which is how the way out is exercised)
+  bool ok = p.wait_cycles >= kLookCycles;
+  if (!ok && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (ok) ok = warp_mbar_wait(bar, parity, abort_flag, p.status, p.wait_cycles);
+    __syncwarp();                                    // (what follows is for whole warps)
+    return ok;
+  };
+  Walk walk(p, blockIdx.x);
+  __syncwarp();
+  if (warp < kKwSumWarps) {
+    // ================================================================== sums: thread = (set, key)
+    const int set = warp >> 2, at128 = tid & 127;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const float2 scale = make_float2(p.scale_log2, p.scale_log2);
+    int job = 0, turn = 0;
+    for (KeyPiece w = next_keys(walk); w.any; w = next_keys(walk)) {
+      const int key = w.key0 + at128, jobs = w.last - w.first;
+      // the rows, counted from the piece's first, that see this key
+      const int2 seen = rows_over(p, w.x, key, 1);
+      const int ra = seen.x - w.row0, rb = min(seen.y - w.row0, w.rows);
+      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      for (int gi = w.first; gi < w.last; ++gi, ++job) {
+        if ((job & 1) != set) continue;
+        const int buf = job % kKwBufs, slot = job % kKwNQ, n = min(kKwRows, w.rows - gi * kKwRows);
+        const int a = ra - gi * kKwRows, b = rb - gi * kKwRows;          // of the job's columns this key counts a .. b - 1
+        const bool part = __any_sync(0xffffffffu, a > 0 || b < n);
+        if (!wait(s_full + 8 * buf, (job / kKwBufs) & 1)) break;
+        tc5_fence_after();
+        const float* norm = norms + slot * kKwRows;
+#pragma unroll 1
+        for (int c = 0; c < n; c += 32) {
+          uint32_t x[32];
+          tc5_ld32_nowait(tmem + buf * 128 + c + lanes, x);
+          tc5_wait_ld();
+          tc5_pin32(x);
+          const uint32_t on = part ? low_bits(b - c) & ~low_bits(a - c) : 0xffffffffu;
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float4 l = *reinterpret_cast<const float4*>(norm + c + k);
+            float2 e = fma2_f32(make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), scale, make_float2(-l.x, -l.y));
+            float2 f = fma2_f32(make_float2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), scale, make_float2(-l.z, -l.w));
+            e.x = ex2(e.x);
+            e.y = ex2(e.y);
+            f.x = ex2(f.x);
+            f.y = ex2(f.y);
+            if (part) {
+              e.x = (on >> k) & 1u ? e.x : 0.f;
+              e.y = (on >> (k + 1)) & 1u ? e.y : 0.f;
+              f.x = (on >> (k + 2)) & 1u ? f.x : 0.f;
+              f.y = (on >> (k + 3)) & 1u ? f.y : 0.f;
+            }
+            sum[0] = add2_f32(sum[0], e);
+            sum[1] = add2_f32(sum[1], f);
+          }
+        }
+        tc5_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(s_free + 8 * buf, 1);
+          mbar_arrive(q_free + 8 * slot, 1);
+        }
+        __syncwarp();
+      }
+      const float2 both = add2_f32(sum[0], sum[1]);
+      float total = both.x + both.y;
+      int writer = jobs == 1 ? (job + 1) & 1 : 0;    // (the set that had the only job; a tile without any is the first one's)
+      if (jobs > 1) {
+        if (set == 1) other[(turn & 1) * kKwKeys + at128] = total;
+        __syncwarp();
+        asm volatile("bar.sync 1, %0;" ::"n"(kKwSumWarps * 32) : "memory");
+        if (set == 0) total += other[(turn & 1) * kKwKeys + at128];
+        ++turn;                                      // (a place is written again after the next meeting, which comes after this reading)
+      }
+      if (set == writer && ok) {
+        if (w.whole()) {
+          if (key < w.x.len) put_weight(p, w.x, w.s, w.kh, key, total);
+        } else {
+          p.partials[record_at(blockIdx.x, w.first == 0) * kKwKeys + at128] = total;
+        }
+      }
+      __syncwarp();
+    }
+  } else if (warp == kKwLoadWarp) {
+    // ================================================================== keys
+    int n = 0;
+    for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
+      if (w.last == w.first) continue;
+      const int slot = n % kKwNK, key = w.key0 + lane * GP;
+      int page = -1;
+      if (lane < PG && key < w.x.len) page = max(0, page_of(p.c, w.s, key / GP, p.status));
+      const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
+      if (n >= kKwNK && !wait(k_free + 8 * slot, (n / kKwNK - 1) & 1)) break;
+      if (elect_one()) mbar_expect_tx(k_full + 8 * slot, __popc(have) * (GP * D * 2));
+      __syncwarp();
+#pragma unroll 1
+      for (int j = 0; j < PG; ++j) {
+        const int from = __shfl_sync(0xffffffffu, page, j);
+        if (from >= 0 && elect_one())
+#pragma unroll
+          for (int h = 0; h < D / 64; ++h) tma_load_page(kring + slot * TILE + h * HS + j * GP * 128, &map_k, k_full + 8 * slot, h * 64, w.kh, from);
+        __syncwarp();
+      }
+      ++n;
+    }
+    // (what is in flight has landed before the CTA's shared memory is given up)
+    if (!ok)
+      for (int i = 0; i < min(kKwNK, n); ++i) mbar_drain(k_full + 8 * i, ((n - 1 - i) / kKwNK) & 1);
+    __syncwarp();
+  } else if (warp == kKwMmaWarp) {
+    // ================================================================== K Q^T
+    const uint32_t kr = warp_uniform(kring), qr = warp_uniform(qring);
+    int job = 0, n = 0;
+    for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
+      if (w.last == w.first) continue;
+      const int kslot = n % kKwNK;
+      if (!wait(k_full + 8 * kslot, (n / kKwNK) & 1)) break;
+      for (int gi = w.first; gi < w.last; ++gi, ++job) {
+        const int buf = job % kKwBufs, slot = job % kKwNQ, cols = min(kKwRows, w.rows - gi * kKwRows);
+        if (!wait(q_full + 8 * slot, (job / kKwNQ) & 1)) break;
+        if (job >= kKwBufs && !wait(s_free + 8 * buf, (job / kKwBufs - 1) & 1)) break;
+        tc5_fence_after();
+        if (elect_one()) {
+          const uint32_t idesc = tc5_idesc(128, (cols + 31) & ~31, 0, 1u, 1u);
+          const uint64_t kd = tc5_desc(kr + kslot * TILE, 16), qd = tc5_desc(qr + slot * TILE, 16);
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t at = ((ks >> 2) * HS + (ks & 3) * 32) / 16;
+            tc5_mma_ss(tmem + buf * 128, kd + at, qd + at, idesc, ks > 0 ? 1u : 0u);
+          }
+          tc5_commit(s_full + 8 * buf);
+          tc5_commit(q_free + 8 * slot);
+          if (gi + 1 == w.last) tc5_commit(k_free + 8 * kslot);
+        }
+        __syncwarp();
+      }
+      ++n;
+    }
+    // the products in flight have run before tensor memory is given back
+    if (elect_one()) {
+      tc5_commit(drain);
+      mbar_drain(drain, 0);
+    }
+    __syncwarp();
+  } else {
+    // ================================================================== rows of Q, sixteen (or eight) lanes to a row
+    constexpr int LPR = D / 8, RPW = 32 / LPR;       // lanes of 16 bytes per row, rows a warp takes at a time
+    const int qw = warp - kKwQWarp, col = lane % LPR, sub = lane / LPR;
+    auto landed = [&](int j, auto still) {           // (one job's copies stay in flight while the next one's are begun)
+      asm volatile("cp.async.wait_group %0;" ::"n"(decltype(still)::value) : "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the products read the tile through the async proxy
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full + 8 * (j % kKwNQ), 1);
+      __syncwarp();
+    };
+    int job = 0;
+    for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
+      for (int gi = w.first; gi < w.last; ++gi, ++job) {
+        const int slot = job % kKwNQ, n = min(kKwRows, w.rows - gi * kKwRows), padded = (n + 31) & ~31;
+        if (job >= kKwNQ && !wait(q_free + 8 * slot, (job / kKwNQ - 1) & 1)) break;
+        uint8_t* tile = gen + (kKwNK + slot) * TILE;
+        const int row0 = w.row0 + gi * kKwRows;
+        for (int i = qw * 32 + lane; i < padded; i += kKwQWarps * 32) {
+          float l = INFINITY;                        // a row that does not exist, or saw nothing, gives nothing
+          if (i < n) {
+            const int t = (row0 + i) / p.c.G;
+            const float v = p.lse[(static_cast<long long>(w.x.cu) + t) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + (row0 + i - t * p.c.G)];
+            l = v == -INFINITY ? INFINITY : v * kLog2e;
+          }
+          norms[slot * kKwRows + i] = l;
+        }
+        for (int i = qw * RPW + sub; i < padded; i += kKwQWarps * RPW) {
+          uint32_t dst = smem_u32(tile + (col >> 3) * HS + tc5_sw(i, col & 7));
+          const int r = i < n ? row0 + i : row0, t = r / p.c.G;
+          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.q) + (static_cast<long long>(w.x.cu) + t) * p.q.stride + (w.kh * p.c.G + r - t * p.c.G) * D + col * 8;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(i < n ? 16 : 0) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (job > 0) landed(job - 1, std::integral_constant<int, 1>{});
+      }
+    }
+    if (job > 0) landed(job - 1, std::integral_constant<int, 0>{});
+  }
+  tc5_fence_before();
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// Tiles that several CTAs share: a thread per key adds their sums, in CTA order.
+__global__ void __launch_bounds__(kKwKeys) weights_join_kernel(const __grid_constant__ WeightParams p) {
+  grid_dep_wait();
+  const int b = blockIdx.x + 1;
+  Share x;
+  const int last = records_from(p, b, x);
+  if (last < b) return;
+  const int key = tile_key(key_reach(p, x.t.x), x.t.j) + threadIdx.x;
+  float total = 0.f;
+  for (int i = b - 1; i <= last; ++i) total += p.partials[record_at(i, i == b - 1) * kKwKeys + threadIdx.x];
+  if (key < x.t.x.len) put_weight(p, x.t.x, x.t.s, x.kh, key, total);
+}

@@ -1,52 +1,30 @@
 // Attention of new tokens over the paged cache with a sliding window and first tokens that stay visible: losa_window_attn.
 //
 // Rows (token, head of a KV head) are taken in tiles; a tile reads the groups of keys that any of its rows sees.  All
-// (tile, KV head, group) form one list, cut into equal shares, one per CTA, so prompts, blocks and single tokens of any lengths fill
-// the GPU alike.  A tile that several CTAs share leaves records (reference, sum, un-normalised output per row) that a kernel of
-// its own merges by log-sum-exp.  A first small kernel writes the list's tiles and where each share begins.
-#include <cuda.h>
-
+// (tile, KV head, group) form one list, cut into equal shares, so prompts, blocks and single tokens of any lengths fill
+// the GPU alike.  A tile that several CTAs share leaves records (reference, sum, un-normalised output per row), joined by log-sum-exp.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
 
-#include "cache_view.cuh"
 #include "kernels.h"
-#include "tcgen05_ops.cuh"
+#include "tc_cache_ops.cuh"
+#include "work_list.cuh"
 
 namespace losa {
 namespace {
 
-// Where a share begins: tile, KV head, position in the (tile, KV head): `pad` positions that stand for no group (entering a tile
-// costs a CTA as much time), then its groups.
-struct Share { int tile, kh, at, unused; };
-struct Tile { int s, j, groups, unused; };           // rows j * R .. of sequence s
-struct Plan {
-  int* head;                                         // [4]: shares, tiles
-  Sequence* seqs;                                    // [N]
-  Share* shares;                                     // [n_ctas + 1]
-  Tile* tiles;
-};
-
-struct WindowParams {
-  CacheParams c;
-  QueryParams q;
-  Plan plan;
+struct WindowParams : ListParams {
   void* out;                                         // [T, H_q, d] dtype
   float* lse;                                        // or null
   float* partials;                                   // [n_ctas][2][R * (d + 2)]
-  int32_t* status;
-  long long max_tiles;                               // room of the plan
-  int n_ctas, pad, least;
   float scale_log2;                                  // sm_scale * log2(e)
-  float sm_scale;
-  long long wait_cycles;
 };
 
-// The groups (of GT keys) that a tile's rows see: the first `first`, then those from `from` on, up to `end` keys.
+// The groups (of GT keys) that rows row0 .. of a sequence see: the first `first`, then those from `from` on, up to `end` keys.
 struct Reach { int first, from, groups, end, lo; };
 template <int GT>
-__device__ __forceinline__ Reach reach_of(const WindowParams& p, const Sequence& x, int row0, int rows) {
+__device__ __forceinline__ Reach reach_of(const ListParams& p, const Sequence& x, int row0, int rows) {
   const int t0 = row0 / p.c.G, t1 = min(x.count - 1, (row0 + rows - 1) / p.c.G);
   Reach r;
   r.end = keys_of(p.q, x, x.start + t1).x;
@@ -59,186 +37,48 @@ __device__ __forceinline__ Reach reach_of(const WindowParams& p, const Sequence&
 }
 template <int GT> __device__ __forceinline__ int group_key(const Reach& r, int i) { return (i < r.first ? i : r.from + i - r.first) * GT; }
 
-// ===================================================================== the list of work
-constexpr int kPlanThreads = 1024;
 template <int R, int GT>
-__global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_constant__ WindowParams p) {
-  __shared__ int before[kPlanThreads + 1];           // tiles before a sequence
-  __shared__ long long sums[kPlanThreads / 32 + 1];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  auto scan = [&](long long v) {                     // exclusive; the total is left in sums[32]
-    long long inc = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += t;
-    }
-    if (lane == 31) sums[warp] = inc;
-    __syncthreads();
-    if (warp == 0) {
-      const long long w = sums[lane];
-      long long winc = w;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, winc, o);
-        if (lane >= o) winc += t;
-      }
-      sums[lane] = winc - w;
-      if (lane == 31) sums[32] = winc;
-    }
-    __syncthreads();
-    const long long out = sums[warp] + inc - v;
-    return out;
-  };
-  grid_dep_trigger();
-  grid_dep_wait();
-  Sequence x = {0, 0, 0, 0};
-  if (tid < p.c.N) {
-    x = sequence_of(p.c, p.q, tid, p.status);
-    p.plan.seqs[tid] = x;
-  }
-  const int mine = static_cast<int>((static_cast<long long>(x.count) * p.c.G + R - 1) / R);
-  const long long tiles_before = scan(mine);
-  const bool fits = sums[32] <= p.max_tiles;         // (sequences that overlap in `cu` can make more tiles than the tokens have)
-  if (!fits && tid == 0) set_status(p.status, LOSA_ERR_BOUNDS);
-  before[tid] = fits ? static_cast<int>(tiles_before) : 0;
-  const int X = fits ? static_cast<int>(sums[32]) : 0;
-  if (tid == 0) before[kPlanThreads] = X;
-  __syncthreads();
-  // every thread: a run of tiles
-  const int per = (X + kPlanThreads - 1) / kPlanThreads, a = min(X, tid * per), z = min(X, a + per);
-  int s = 0;
-  if (a < z) {
-    int b = kPlanThreads;                            // before[s] <= a < before[b]
-    while (b - s > 1) {
-      const int m = (s + b) >> 1;
-      if (before[m] <= a) s = m; else b = m;
-    }
-  }
-  long long sum = 0;
-  Sequence y = {0, 0, 0, 0};
-  int have = -1, at = s;
-  for (int t = a; t < z; ++t) {
-    while (before[at + 1] <= t) ++at;
-    if (at != have) { y = p.plan.seqs[at]; have = at; }
-    const int j = t - before[at];
-    const int n = reach_of<GT>(p, y, j * R, R).groups;
-    p.plan.tiles[t] = {at, j, n, 0};
-    sum += p.pad + n;
-  }
-  __syncthreads();
-  long long pos = scan(sum) * p.c.Hkv;
-  const long long total = sums[32] * p.c.Hkv;
-  const int n = static_cast<int>(max(1ll, min(static_cast<long long>(p.n_ctas), total / p.least)));
-  auto lo = [&](long long b) { return cta_lo(total, static_cast<int>(b), n); };
-  for (int t = a; t < z; ++t) {
-    const int length = p.pad + p.plan.tiles[t].groups;
-    const long long end = pos + static_cast<long long>(length) * p.c.Hkv;
-    long long b = pos * n / total;                   // shares that begin in this tile
-    while (b > 0 && lo(b - 1) >= pos) --b;
-    while (b < n && lo(b) < pos) ++b;
-    for (; b < n && lo(b) < end; ++b) {
-      const int off = static_cast<int>(lo(b) - pos);
-      p.plan.shares[b] = {t, off / length, off % length, 0};
-    }
-    pos = end;
-  }
-  if (tid == 0) {
-    p.plan.head[0] = X > 0 ? n : 0;
-    p.plan.head[1] = X;
-    p.plan.shares[X > 0 ? n : 0] = {X, 0, 0, 0};
-  }
-}
-
-// A CTA's part of one (tile, KV head).
-struct Piece {
-  int tile, kh, s, row0, rows;                       // rows: that exist
-  int first, last, groups;                           // groups first .. last - 1 of `groups`
-  Sequence x;
+struct RowTiles {
+  static __device__ __forceinline__ int tiles(const ListParams& p, const Sequence& x) { return static_cast<int>((static_cast<long long>(x.count) * p.c.G + R - 1) / R); }
+  static __device__ __forceinline__ int groups(const ListParams& p, const Sequence& x, int j) { return reach_of<GT>(p, x, j * R, R).groups; }
+};
+struct Piece : Part {
+  int row0, rows;                                    // rows: that exist
   Reach r;
-  bool any;                                          // false: the share is at its end
-  __device__ __forceinline__ bool whole() const { return first == 0 && last == groups; }
 };
 template <int R, int GT>
-struct Walk {
-  const WindowParams& p;
-  Share at, end;                                     // next position, the share's end
-  __device__ __forceinline__ Walk(const WindowParams& params, int b) : p(params) {
-    const int n = p.plan.head[0];
-    if (b >= n) {
-      at = end = {0, 0, 0, 0};
-      return;
-    }
-    at = p.plan.shares[b];
-    end = p.plan.shares[b + 1];
+__device__ __forceinline__ Piece next_piece(Walk& walk) {
+  Piece w;
+  static_cast<Part&>(w) = walk.next();
+  if (w.any) {
+    w.row0 = w.j * R;
+    w.rows = min(R, w.x.count * walk.p.c.G - w.row0);
+    w.r = reach_of<GT>(walk.p, w.x, w.row0, R);
   }
-  __device__ __forceinline__ bool done() const { return at.tile == end.tile && at.kh == end.kh && at.at == end.at; }
-  // the next piece that has groups, or that stands for a tile without any (whose results are those of no key)
-  __device__ __forceinline__ Piece next() {
-    Piece w;
-    w.any = false;
-    while (!done()) {
-      const Tile t = p.plan.tiles[at.tile];
-      const int length = p.pad + t.groups;
-      const bool cut = at.tile == end.tile && at.kh == end.kh;
-      const int from = at.at, to = cut ? end.at : length;
-      w.tile = at.tile;
-      w.kh = at.kh;
-      w.s = t.s;
-      w.groups = t.groups;
-      w.first = max(0, from - p.pad);
-      w.last = max(0, to - p.pad);
-      const bool begins = from == 0;
-      if (cut) at = end;
-      else if (at.kh + 1 < p.c.Hkv) at = {at.tile, at.kh + 1, 0, 0};
-      else at = {at.tile + 1, 0, 0, 0};
-      if (w.last > w.first || (t.groups == 0 && begins)) {
-        w.x = p.plan.seqs[t.s];
-        w.row0 = t.j * R;
-        w.rows = min(R, w.x.count * p.c.G - w.row0);
-        w.r = reach_of<GT>(p, w.x, w.row0, R);
-        w.any = true;
-        break;
-      }
-    }
-    return w;
-  }
-};
+  return w;
+}
 // row of q / out (in units of d elements) of row r of a piece
-__device__ __forceinline__ long long token_head(const WindowParams& p, const Piece& w, int r) {
+__device__ __forceinline__ long long token_head(const ListParams& p, const Piece& w, int r) {
   const int row = w.row0 + r, t = row / p.c.G;
   return (static_cast<long long>(w.x.cu) + t) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + (row - t * p.c.G);
 }
-// the record of a piece: the first piece of a tile in its CTA's second place, the others (their CTA's first piece) in the first
 template <int R, int D>
-__device__ __forceinline__ float* record_of(const WindowParams& p, int b, bool first) {
-  return p.partials + (static_cast<size_t>(b) * 2 + (first ? 1 : 0)) * (R * (D + 2));
-}
+__device__ __forceinline__ float* record_of(const WindowParams& p, int b, bool first) { return p.partials + record_at(b, first) * (R * (D + 2)); }
 
-// Tiles that several CTAs share: a warp per row merges their records, in CTA order.  Block (b, .) looks after the tile that share b
-// begins in, if it is the first share to begin among that tile's groups.
+// Tiles that several CTAs share: a warp per row joins their records.  Blocks (b, .): the tile that share b begins in.
 constexpr int kMergeWarps = 8;
 template <int R, int D, typename T>
 __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __grid_constant__ WindowParams p) {
   grid_dep_wait();
   const int b = blockIdx.x + 1, lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
-  const int n = p.plan.head[0];
-  if (b >= n) return;
-  const Share x = p.plan.shares[b], prev = p.plan.shares[b - 1];
-  if (x.at <= p.pad) return;                         // cut before its first group: it is whole in this CTA, or the next one's
-  if (prev.tile == x.tile && prev.kh == x.kh && prev.at > p.pad) return;
-  const Tile t = p.plan.tiles[x.tile];
+  Share x;
+  const int last = records_from(p, b, x);
+  if (last < b) return;
   Piece w;
-  w.x = p.plan.seqs[t.s];
+  w.x = x.t.x;
   w.kh = x.kh;
-  w.row0 = t.j * R;
+  w.row0 = x.t.j * R;
   if (r >= w.x.count * p.c.G - w.row0) return;
-  int last = b;
-  while (last + 1 < n) {
-    const Share y = p.plan.shares[last + 1];
-    if (y.tile != x.tile || y.kh != x.kh) break;
-    ++last;
-  }
   constexpr int C = D / 32, kBatch = 4;
   float acc[C], M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -293,14 +133,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __
 // ===================================================================== host side
 template <int R, int GT, int D, typename Launch, typename T>
 int32_t with_plan(losa_ctx* c, WindowParams& p, cudaStream_t st, T, Launch&& main_kernel) {
-  char* at = c->ws + c->lay.plan;
-  p.plan.head = reinterpret_cast<int*>(at);
-  p.plan.seqs = reinterpret_cast<Sequence*>(at + 256);
-  p.plan.shares = reinterpret_cast<Share*>(at + 256 + sizeof(Sequence) * c->shape.batch);
-  p.plan.tiles = reinterpret_cast<Tile*>(p.plan.shares + p.n_ctas + 1);
-  p.max_tiles = c->lay.plan_tiles;
+  place_plan(c, p);
   p.partials = reinterpret_cast<float*>(c->ws + c->lay.scores);
-  launch_k(window_plan_kernel<R, GT>, 1, kPlanThreads, 0, st, p);
+  launch_k(list_plan_kernel<RowTiles<R, GT>>, 1, kPlanThreads, 0, st, static_cast<const ListParams&>(p));
   int32_t rc = after_launch(c);
   if (rc == LOSA_OK) rc = main_kernel();
   if (rc != LOSA_OK) return rc;
@@ -357,7 +192,6 @@ int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t
   p.out = out;
   p.lse = lse_opt;
   p.status = status_ptr(c);
-  p.sm_scale = c->shape.sm_scale;
   p.scale_log2 = c->shape.sm_scale * kLog2e;
   p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
   auto run = [&](auto f) {

@@ -16,8 +16,8 @@ __global__ void __launch_bounds__(kWinThreads, 2) window_f32_kernel(const __grid
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   grid_dep_trigger();
   grid_dep_wait();
-  Walk<R, GT> walk(p, blockIdx.x);
-  for (Piece w = walk.next(); w.any; w = walk.next()) {
+  Walk walk(p, blockIdx.x);
+  for (Piece w = next_piece<R, GT>(walk); w.any; w = next_piece<R, GT>(walk)) {
     __syncthreads();
     for (int i = tid; i < R * C8; i += kWinThreads) {
       const int r = i / C8, ch = i - r * C8;

@@ -24,37 +24,10 @@ constexpr float kWtTau = 8.f, kWtFused = 1048576.f;  // a reference up to this: 
 template <int D> constexpr int wt_tile() { return kWtKeys * D * 2; }
 template <int D> constexpr int wt_smem() { return 1024 + 2 * 128 * D * 2 + (kWtNK + kWtNV) * wt_tile<D>() + 512; }
 
-__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, uint32_t bar, int col, int head, int page) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-               ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(0), "r"(head), "r"(page) : "memory");
-}
 __device__ __forceinline__ void wt_store16(void* at, bool on, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p st.global.v4.b32 [%0], {%2, %3, %4, %5};\n\t}"
                ::"l"(at), "r"(static_cast<int>(on)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ float wt_max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-__device__ __forceinline__ float2 wt_fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 wt_add2(float2 a, float2 b) {
-  float2 c;
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return c;
-}
-__device__ __forceinline__ uint32_t wt_pack(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
-
 // What the rows of a piece have in common: every row sees the keys below `end`, from `lo` on or below the sinks.
 struct Common { int end, lo; bool same; };
 __device__ __forceinline__ Common common_of(const WindowParams& p, const Piece& w) {
@@ -131,7 +104,8 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
     __syncwarp();                                    // (what follows is for whole warps)
     return ok;
   };
-  Walk<R, GT> walk(p, blockIdx.x);
+  Walk walk(p, blockIdx.x);
+  auto next = [&]() { return next_piece<R, GT>(walk); };
 
   __syncwarp();
   if (warp < kWtSoftWarps) {
@@ -163,7 +137,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full + 8 * set, 1);
     };
-    Piece w = walk.next();
+    Piece w = next();
     write_q(w);
     int n = 0, pieces = 0;                           // jobs of this set before; pieces with groups so far
     const float sc = p.scale_log2;
@@ -200,8 +174,8 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
           float top = kWtNone, top2 = kWtNone;
 #pragma unroll
           for (int k = 0; k < 128; k += 4) {
-            top = wt_max3(top, score(k), score(k + 1));
-            top2 = wt_max3(top2, score(k + 2), score(k + 3));
+            top = max3_f32(top, score(k), score(k + 1));
+            top2 = max3_f32(top2, score(k + 2), score(k + 3));
           }
           top = fmaxf(top, top2);
           const bool grow = (top - m) * sc > kWtTau || m == kWtNone;       // (none yet: whatever the scale)
@@ -234,11 +208,11 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
             uint32_t h[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-              float2 e = wt_fma2(make_float2(score(c * 32 + 2 * k), score(c * 32 + 2 * k + 1)), scale, sh);
+              float2 e = fma2_f32(make_float2(score(c * 32 + 2 * k), score(c * 32 + 2 * k + 1)), scale, sh);
               e.x = ex2(e.x);
               e.y = ex2(e.y);
-              sum[k & 1] = wt_add2(sum[k & 1], e);
-              h[k] = wt_pack(e.x, e.y);
+              sum[k & 1] = add2_f32(sum[k & 1], e);
+              h[k] = pack_b16(e.x, e.y);
             }
             tc5_st16(s_at + c * 16, h);
             if (c & 1) {
@@ -249,7 +223,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
               __syncwarp();
             }
           }
-          sum[0] = wt_add2(sum[0], sum[1]);
+          sum[0] = add2_f32(sum[0], sum[1]);
           l += sum[0].x + sum[0].y;
         } else {
           tc5_fence_before();
@@ -281,7 +255,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
         if (top == -INFINITY) L = xl[at128] + xl[128 + at128];       // (zero, or no number, which stays visible)
       }
       tc5_fence_after();
-      const Piece following = walk.next();
+      const Piece following = next();
       const bool q_now = !both || joint(following);      // (else the exchange lies where the second tile goes)
       if (q_now) write_q(following);
       if (filled(w)) ++pieces;
@@ -338,7 +312,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + out_row * D + c * 16;
 #pragma unroll
             for (int k = 0; k < 16; k += 8)
-              wt_store16(out + k, on, wt_pack(x[k] * inv, x[k + 1] * inv), wt_pack(x[k + 2] * inv, x[k + 3] * inv), wt_pack(x[k + 4] * inv, x[k + 5] * inv), wt_pack(x[k + 6] * inv, x[k + 7] * inv));
+              wt_store16(out + k, on, pack_b16(x[k] * inv, x[k + 1] * inv), pack_b16(x[k + 2] * inv, x[k + 3] * inv), pack_b16(x[k + 4] * inv, x[k + 5] * inv), pack_b16(x[k + 6] * inv, x[k + 7] * inv));
           }
           __syncwarp();
         }
@@ -364,7 +338,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
     if (warp == kWtLoadWarp) {
       // ================================================================== pages
       int g = 0, nk = 0, nv = 0;                     // groups; copies begun
-      for (Piece w = walk.next(); w.any && ok; w = walk.next()) {
+      for (Piece w = next(); w.any && ok; w = next()) {
         int pages = 0;                               // of the next 32 / PG groups, one per lane; -1: nobody sees it
         for (int gi = w.first; gi < w.last; ++gi, ++g) {
           const int i = (gi - w.first) % (32 / PG);
@@ -413,7 +387,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       // ================================================================== Q K^T
       const uint32_t qt = warp_uniform(qtile), kr = warp_uniform(kring), idesc = tc5_idesc(128, GT, 0, 1u, 1u);
       int g = 0, n[2] = {0, 0}, q0 = 0, q1 = 0;
-      for (Piece w = walk.next(); w.any && ok; w = walk.next()) {
+      for (Piece w = next(); w.any && ok; w = next()) {
         const bool both = joint(w);
         if (!filled(w)) continue;
         wait(q_full, q0++ & 1);
@@ -445,7 +419,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       // ================================================================== P V
       const uint32_t vr = warp_uniform(vring), idesc = tc5_idesc(128, D, 1, 1u, 1u);
       int g = 0, n[2] = {0, 0}, piece = 0;
-      for (Piece w = walk.next(); w.any && ok; w = walk.next()) {
+      for (Piece w = next(); w.any && ok; w = next()) {
         const bool both = joint(w);
         if (!filled(w)) continue;
         if (piece++ > 0) {
@@ -482,7 +456,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
     } else {
       // ================================================================== values that must not count
       int g = 0, pieces = 0;
-      for (Piece w = walk.next(); w.any && ok; w = walk.next()) {
+      for (Piece w = next(); w.any && ok; w = next()) {
         const Common com = common_of(p, w);
         if (filled(w)) ++pieces;
         for (int gi = w.first; gi < w.last; ++gi, ++g) {
