@@ -40,35 +40,42 @@ __device__ __forceinline__ void put_weight(const WeightParams& p, const Sequence
 #include "kv_weights_f32.cuh"
 #include "kv_weights_tc.cuh"
 
-template <int FMT, int D>
-int32_t launch(losa_ctx* c, const WeightParams& p, cudaStream_t st) {
-  auto kernel = weights_f32_kernel<FMT, D>;
-  LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, weights_smem<D>()));
+template <int D>
+int32_t launch_f32(losa_ctx* c, const WeightParams& p, cudaStream_t st) {
+  auto kernel = weights_f32_kernel<D>;
+  constexpr int bit = 16 << kRowsF32;
+  if (!(c->window_attr_set & bit)) {
+    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, weights_smem<D>()));
+    c->window_attr_set |= bit;
+  }
   const int tiles = (p.c.Pmax * p.c.g + kWgtKeys - 1) / kWgtKeys;
   if (tiles == 0) return LOSA_OK;
   launch_k(kernel, dim3(tiles, p.c.Hkv, p.c.N), kWgtThreads, weights_smem<D>(), st, p);
   return after_launch(c);
 }
 
-template <int D, int GP>
+template <int FMT, int D, int GP>
 int32_t launch_tc(losa_ctx* c, WeightParams& p, const losa_kv_t* kv, cudaStream_t st) {
-  const int32_t rc = pool_tensor_maps(c, kv);
-  if (rc != LOSA_OK) return rc;
-  CUtensorMap mk;
-  memcpy(&mk, c->tmap_k, sizeof(mk));
+  using Tc = WeightsTc<FMT, D, GP>;
+  CUtensorMap mk = {};
+  if constexpr (!Tc::quant) {
+    const int32_t rc = pool_tensor_maps(c, kv);
+    if (rc != LOSA_OK) return rc;
+    memcpy(&mk, c->tmap_k, sizeof(mk));
+  }
   p.n_ctas = c->n_sms;
   p.pad = 1;
   p.least = 2;
   place_plan(c, p);
   p.partials = reinterpret_cast<float*>(c->ws + c->lay.scores);
-  auto kernel = weights_tc_kernel<D, GP>;
-  if (!(c->window_attr_set & 2)) {
-    static_assert(kw_smem<D>() <= 232448, "shared memory");
-    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kw_smem<D>()));
-    c->window_attr_set |= 2;
+  auto kernel = weights_tc_kernel<FMT, D, GP>;
+  constexpr int bit = 16 << FMT;
+  if (!(c->window_attr_set & bit)) {
+    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc::smem));
+    c->window_attr_set |= bit;
   }
   launch_k(list_plan_kernel<KeyTiles>, 1, kPlanThreads, 0, st, static_cast<const ListParams&>(p));
-  launch_k(kernel, p.n_ctas, kKwWarps * 32, kw_smem<D>(), st, mk, p);
+  launch_k(kernel, p.n_ctas, kKwWarps * 32, Tc::smem, st, mk, p);
   launch_k(weights_join_kernel, p.n_ctas, kKwKeys, 0, st, p);
   return after_launch(c, 3);
 }
@@ -85,21 +92,20 @@ int32_t launch_kv_weights(losa_ctx* c, const losa_queries_t* q, const losa_kv_t*
   p.status = status_ptr(c);
   p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
   p.scale_log2 = c->shape.sm_scale * kLog2e;
-  auto run = [&](auto f) {
-    constexpr int FMT = decltype(f)::value;
-    return c->shape.head_dim == 128 ? launch<FMT, 128>(c, p, st) : launch<FMT, 64>(c, p, st);
-  };
-  switch (row_format(c, kv)) {
-    case kRowsF32: return run(std::integral_constant<int, kRowsF32>{});
-    case kRowsBf16: {
-      auto with_page = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        return c->shape.page_size == 16 ? launch_tc<D, 16>(c, p, kv, st) : c->shape.page_size == 32 ? launch_tc<D, 32>(c, p, kv, st) : launch_tc<D, 64>(c, p, kv, st);
-      };
-      return c->shape.head_dim == 128 ? with_page(std::integral_constant<int, 128>{}) : with_page(std::integral_constant<int, 64>{});
+  auto run = [&](auto f, auto d) -> int32_t {
+    constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
+    if constexpr (FMT == kRowsF32) {
+      return launch_f32<D>(c, p, st);
+    } else {
+      return c->shape.page_size == 16 ? launch_tc<FMT, D, 16>(c, p, kv, st) : c->shape.page_size == 32 ? launch_tc<FMT, D, 32>(c, p, kv, st) : launch_tc<FMT, D, 64>(c, p, kv, st);
     }
-    case kRowsFp8: return run(std::integral_constant<int, kRowsFp8>{});
-    default: return run(std::integral_constant<int, kRowsInt4>{});
+  };
+  auto with_dim = [&](auto f) { return c->shape.head_dim == 128 ? run(f, std::integral_constant<int, 128>{}) : run(f, std::integral_constant<int, 64>{}); };
+  switch (row_format(c, kv)) {
+    case kRowsF32: return with_dim(std::integral_constant<int, kRowsF32>{});
+    case kRowsBf16: return with_dim(std::integral_constant<int, kRowsBf16>{});
+    case kRowsFp8: return with_dim(std::integral_constant<int, kRowsFp8>{});
+    default: return with_dim(std::integral_constant<int, kRowsInt4>{});
   }
 }
 

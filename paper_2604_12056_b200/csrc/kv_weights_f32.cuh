@@ -6,9 +6,9 @@
 constexpr int kWgtKeys = 64, kWgtRows = 64, kWgtThreads = 128;
 template <int D> constexpr int weights_smem() { return (kWgtRows * D + kWgtKeys * (D + 4) + 3 * kWgtRows + 8 * kWgtKeys) * 4; }
 
-template <int FMT, int D>
+template <int D>
 __global__ void __launch_bounds__(kWgtThreads, 3) weights_f32_kernel(const __grid_constant__ WeightParams p) {
-  using T = typename RowFormat<FMT>::Query;
+  using T = float;
   constexpr int R = kWgtRows, GT = kWgtKeys, KS = D + 4, C8 = D / 8;
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sk = sq + R * D, *sl = sk + GT * KS, *part = sl + R;
@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(kWgtThreads, 3) weights_f32_kernel(const __gri
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = 0.f;
       const int page = key < x.len ? page_of(p.c, s, key / p.c.g, p.status) : -1;
-      if (page >= 0) cache_load8<FMT, D>(p.c, p.c.k_pages, p.c.k_scale, page, kh, key % p.c.g, ch, v);
+      if (page >= 0) cache_load8<kRowsF32, D>(p.c, p.c.k_pages, p.c.k_scale, page, kh, key % p.c.g, ch, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) sk[t * KS + ch * 8 + k] = v[k];
     }

@@ -9,10 +9,17 @@
 // A key is seen by a run of rows, so a job that is not seen whole is masked by two numbers per thread.
 #pragma once
 
-constexpr int kKwKeys = 128, kKwRows = 128, kKwBufs = 4, kKwNK = 3, kKwNQ = 3;
-constexpr int kKwSumWarps = 8, kKwLoadWarp = 8, kKwMmaWarp = 9, kKwQWarp = 10, kKwQWarps = 6, kKwWarps = 16;
-template <int D> constexpr int kw_tile() { return 128 * D * 2; }
-template <int D> constexpr int kw_smem() { return 1024 + (kKwNK + kKwNQ) * kw_tile<D>() + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4 + 256; }
+constexpr int kKwKeys = 128, kKwRows = 128, kKwBufs = 4;
+constexpr int kKwSumWarps = 8, kKwLoadWarp = 8, kKwMmaWarp = 9, kKwQWarp = 10, kKwWarps = 16;
+template <int FMT, int D, int GP> struct WeightsTc {
+  static constexpr bool quant = FMT != kRowsBf16;
+  static constexpr int q_warps = quant ? 2 : 6, convert_warp = kKwQWarp + q_warps;       // quantised pages: the last four warps turn them into operands
+  static constexpr int nk = quant ? 2 : 3, nq = 3, nr = 3;       // tiles of keys, of rows; of keys as they lie
+  static constexpr int tile = 128 * D * 2, raw = quant ? RawTile<FMT, D, GP>::bytes : 0;
+  static constexpr int norms = (nk + nq) * tile + (quant ? nr * raw : 0), other = norms + nq * kKwRows * 4, tail = other + 2 * kKwKeys * 4;
+  static constexpr int smem = 1024 + tail + 256;
+  static_assert(smem <= 232448, "shared memory");
+};
 
 // Tiles of keys that have anything to do: those under the first tokens, and from the window of the first token on; all where weights are forgotten.
 struct KeyReach { int first, from, tiles; };
@@ -51,29 +58,34 @@ __device__ __forceinline__ KeyPiece next_keys(Walk& walk) {
   return w;
 }
 
-template <int D, int GP>
+template <int FMT, int D, int GP>
 __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeightParams p) {
-  constexpr int TILE = kw_tile<D>(), HS = 128 * 128, PG = kKwKeys / GP;
+  using Tc = WeightsTc<FMT, D, GP>;
+  constexpr bool QUANT = Tc::quant;
+  constexpr int TILE = Tc::tile, HS = 128 * 128, PG = kKwKeys / GP, NK = Tc::nk, NQ = Tc::nq, NR = Tc::nr;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t kring = base, qring = kring + kKwNK * TILE;
-  constexpr int TAIL = (kKwNK + kKwNQ) * TILE;
-  float* norms = reinterpret_cast<float*>(gen + TAIL);                   // [slot][row] log-normaliser in log2 units
-  float* other = norms + kKwNQ * kKwRows;                                // [2][key] the second set's sums, by turns
-  const uint32_t bars = base + TAIL + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4;
-  const uint32_t k_full = bars, k_free = k_full + 8 * kKwNK, q_full = k_free + 8 * kKwNK, q_free = q_full + 8 * kKwNQ;
-  const uint32_t s_full = q_free + 8 * kKwNQ, s_free = s_full + 8 * kKwBufs, drain = s_free + 8 * kKwBufs;
-  constexpr int MISC = TAIL + kKwNQ * kKwRows * 4 + 2 * kKwKeys * 4 + 8 * (2 * kKwNK + 2 * kKwNQ + 2 * kKwBufs + 1);
-  static_assert(MISC + 8 - TAIL - kKwNQ * kKwRows * 4 - 2 * kKwKeys * 4 <= 256, "barriers");
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + MISC);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + MISC + 4);
+  const uint32_t kring = base, qring = kring + NK * TILE;
+  [[maybe_unused]] constexpr int RAW = (NK + NQ) * TILE;                 // quantised pages as they lie
+  float* norms = reinterpret_cast<float*>(gen + Tc::norms);              // [slot][row] log-normaliser in log2 units
+  float* other = reinterpret_cast<float*>(gen + Tc::other);              // [2][key] the second set's sums, by turns
+  const uint32_t bars = base + Tc::tail;
+  const uint32_t k_full = bars, k_free = k_full + 8 * NK, q_full = k_free + 8 * NK, q_free = q_full + 8 * NQ;
+  const uint32_t s_full = q_free + 8 * NQ, s_free = s_full + 8 * kKwBufs, drain = s_free + 8 * kKwBufs;
+  [[maybe_unused]] const uint32_t r_full = drain + 8, r_free = r_full + 8 * NR;
+  constexpr int MISC = 8 * (2 * NK + 2 * NQ + 2 * kKwBufs + 1 + 2 * NR);
+  static_assert(MISC + 8 <= 256, "barriers");
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + Tc::tail + MISC);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + Tc::tail + MISC + 4);
   const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
 
   grid_dep_trigger();
   if (tid == 0) {
-    for (int i = 0; i < kKwNK; ++i) { mbar_init(k_full + 8 * i, 1); mbar_init(k_free + 8 * i, 1); }
-    for (int i = 0; i < kKwNQ; ++i) { mbar_init(q_full + 8 * i, kKwQWarps); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
+    for (int i = 0; i < NK; ++i) { mbar_init(k_full + 8 * i, QUANT ? 4 : 1); mbar_init(k_free + 8 * i, 1); }
+    if constexpr (QUANT)
+      for (int i = 0; i < NR; ++i) { mbar_init(r_full + 8 * i, 32); mbar_init(r_free + 8 * i, 4); }
+    for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, Tc::q_warps); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
     for (int i = 0; i < kKwBufs; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_free + 8 * i, 4); }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -115,7 +127,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
         if ((job & 1) != set) continue;
-        const int buf = job % kKwBufs, slot = job % kKwNQ, n = min(kKwRows, w.rows - gi * kKwRows);
+        const int buf = job % kKwBufs, slot = job % NQ, n = min(kKwRows, w.rows - gi * kKwRows);
         const int a = ra - gi * kKwRows, b = rb - gi * kKwRows;          // of the job's columns this key counts a .. b - 1
         const bool part = __any_sync(0xffffffffu, a > 0 || b < n);
         if (!wait(s_full + 8 * buf, (job / kKwBufs) & 1)) break;
@@ -179,11 +191,18 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
     int n = 0;
     for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
       if (w.last == w.first) continue;
-      const int slot = n % kKwNK, key = w.key0 + lane * GP;
+      const int slot = n % (QUANT ? NR : NK), key = w.key0 + lane * GP;
       int page = -1;
       if (lane < PG && key < w.x.len) page = max(0, page_of(p.c, w.s, key / GP, p.status));
+      __syncwarp();
+      if constexpr (QUANT) {
+        if (n >= NR && !wait(r_free + 8 * slot, (n / NR - 1) & 1)) break;
+        raw_load<FMT, D, GP>(p.c, p.c.k_pages, p.c.k_scale, w.kh, page, 0, base + RAW + slot * Tc::raw, r_full + 8 * slot);
+        ++n;
+        continue;
+      }
       const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
-      if (n >= kKwNK && !wait(k_free + 8 * slot, (n / kKwNK - 1) & 1)) break;
+      if (n >= NK && !wait(k_free + 8 * slot, (n / NK - 1) & 1)) break;
       if (elect_one()) mbar_expect_tx(k_full + 8 * slot, __popc(have) * (GP * D * 2));
       __syncwarp();
 #pragma unroll 1
@@ -197,8 +216,9 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       ++n;
     }
     // (what is in flight has landed before the CTA's shared memory is given up)
-    if (!ok)
-      for (int i = 0; i < min(kKwNK, n); ++i) mbar_drain(k_full + 8 * i, ((n - 1 - i) / kKwNK) & 1);
+    if constexpr (QUANT) asm volatile("cp.async.wait_all;" ::: "memory");
+    else if (!ok)
+      for (int i = 0; i < min(NK, n); ++i) mbar_drain(k_full + 8 * i, ((n - 1 - i) / NK) & 1);
     __syncwarp();
   } else if (warp == kKwMmaWarp) {
     // ================================================================== K Q^T
@@ -206,11 +226,11 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
     int job = 0, n = 0;
     for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
       if (w.last == w.first) continue;
-      const int kslot = n % kKwNK;
-      if (!wait(k_full + 8 * kslot, (n / kKwNK) & 1)) break;
+      const int kslot = n % NK;
+      if (!wait(k_full + 8 * kslot, (n / NK) & 1)) break;
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
-        const int buf = job % kKwBufs, slot = job % kKwNQ, cols = min(kKwRows, w.rows - gi * kKwRows);
-        if (!wait(q_full + 8 * slot, (job / kKwNQ) & 1)) break;
+        const int buf = job % kKwBufs, slot = job % NQ, cols = min(kKwRows, w.rows - gi * kKwRows);
+        if (!wait(q_full + 8 * slot, (job / NQ) & 1)) break;
         if (job >= kKwBufs && !wait(s_free + 8 * buf, (job / kKwBufs - 1) & 1)) break;
         tc5_fence_after();
         if (elect_one()) {
@@ -235,6 +255,26 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       mbar_drain(drain, 0);
     }
     __syncwarp();
+  } else if (QUANT && warp >= Tc::convert_warp) {
+    // ================================================================== quantised pages into operands
+    if constexpr (QUANT) {
+      int n = 0;
+      for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
+        if (w.last == w.first) continue;
+        const int slot = n % NR, to = n % NK;
+        if (!wait(r_full + 8 * slot, (n / NR) & 1)) break;
+        if (n >= NK && !wait(k_free + 8 * to, (n / NK - 1) & 1)) break;
+        raw_convert<FMT, D, GP>(gen + RAW + slot * Tc::raw, gen + to * TILE, tid - Tc::convert_warp * 32);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the products read the tile through the async proxy
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(k_full + 8 * to, 1);
+          mbar_arrive(r_free + 8 * slot, 1);
+        }
+        __syncwarp();
+        ++n;
+      }
+    }
   } else {
     // ================================================================== rows of Q, sixteen (or eight) lanes to a row
     constexpr int LPR = D / 8, RPW = 32 / LPR;       // lanes of 16 bytes per row, rows a warp takes at a time
@@ -243,17 +283,17 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       asm volatile("cp.async.wait_group %0;" ::"n"(decltype(still)::value) : "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the products read the tile through the async proxy
       __syncwarp();
-      if (lane == 0) mbar_arrive(q_full + 8 * (j % kKwNQ), 1);
+      if (lane == 0) mbar_arrive(q_full + 8 * (j % NQ), 1);
       __syncwarp();
     };
     int job = 0;
     for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
-        const int slot = job % kKwNQ, n = min(kKwRows, w.rows - gi * kKwRows), padded = (n + 31) & ~31;
-        if (job >= kKwNQ && !wait(q_free + 8 * slot, (job / kKwNQ - 1) & 1)) break;
-        uint8_t* tile = gen + (kKwNK + slot) * TILE;
+        const int slot = job % NQ, n = min(kKwRows, w.rows - gi * kKwRows), padded = (n + 31) & ~31;
+        if (job >= NQ && !wait(q_free + 8 * slot, (job / NQ - 1) & 1)) break;
+        uint8_t* tile = gen + (NK + slot) * TILE;
         const int row0 = w.row0 + gi * kKwRows;
-        for (int i = qw * 32 + lane; i < padded; i += kKwQWarps * 32) {
+        for (int i = qw * 32 + lane; i < padded; i += Tc::q_warps * 32) {
           float l = INFINITY;                        // a row that does not exist, or saw nothing, gives nothing
           if (i < n) {
             const int t = (row0 + i) / p.c.G;
@@ -262,7 +302,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
           }
           norms[slot * kKwRows + i] = l;
         }
-        for (int i = qw * RPW + sub; i < padded; i += kKwQWarps * RPW) {
+        for (int i = qw * RPW + sub; i < padded; i += Tc::q_warps * RPW) {
           uint32_t dst = smem_u32(tile + (col >> 3) * HS + tc5_sw(i, col & 7));
           const int r = i < n ? row0 + i : row0, t = r / p.c.G;
           const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.q) + (static_cast<long long>(w.x.cu) + t) * p.q.stride + (w.kh * p.c.G + r - t * p.c.G) * D + col * 8;

@@ -143,42 +143,48 @@ int32_t with_plan(losa_ctx* c, WindowParams& p, cudaStream_t st, T, Launch&& mai
   return after_launch(c);
 }
 
-template <int FMT, int D>
-int32_t launch_rows(losa_ctx* c, WindowParams& p, cudaStream_t st) {
+template <int D>
+int32_t launch_f32(losa_ctx* c, WindowParams& p, cudaStream_t st) {
   p.n_ctas = 2 * c->n_sms;
   p.pad = 1;
   p.least = 2;
-  using T = typename RowFormat<FMT>::Query;
-  return with_plan<kWinRows, kWinKeys, D>(c, p, st, T{}, [&]() -> int32_t {
-    auto kernel = window_f32_kernel<FMT, D>;
+  auto kernel = window_f32_kernel<D>;
+  constexpr int bit = 1 << kRowsF32;
+  if (!(c->window_attr_set & bit)) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, win_smem<D>()));
+    c->window_attr_set |= bit;
+  }
+  return with_plan<kWinRows, kWinKeys, D>(c, p, st, float{}, [&]() -> int32_t {
     launch_k(kernel, p.n_ctas, kWinThreads, win_smem<D>(), st, p);
     return after_launch(c);
   });
 }
 
-template <int D, int GP>
+template <int FMT, int D, int GP>
 int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_t st) {
-  const int32_t rc = pool_tensor_maps(c, kv);
-  if (rc != LOSA_OK) return rc;
-  CUtensorMap mk, mv;
-  memcpy(&mk, c->tmap_k, sizeof(mk));
-  memcpy(&mv, c->tmap_v, sizeof(mv));
+  using Tc = WindowTc<FMT, D, GP>;
+  CUtensorMap mk = {}, mv = {};
+  if constexpr (!Tc::quant) {
+    const int32_t rc = pool_tensor_maps(c, kv);
+    if (rc != LOSA_OK) return rc;
+    memcpy(&mk, c->tmap_k, sizeof(mk));
+    memcpy(&mv, c->tmap_v, sizeof(mv));
+  }
   p.n_ctas = c->n_sms;
   p.pad = 2;
   p.least = 3;
-  auto kernel = window_tc_kernel<D, GP>;
-  if (!(c->window_attr_set & 1)) {
-    static_assert(wt_smem<D>() <= 232448, "shared memory");
-    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wt_smem<D>()));
+  auto kernel = window_tc_kernel<FMT, D, GP>;
+  constexpr int bit = 1 << FMT;
+  if (!(c->window_attr_set & bit)) {
+    LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc::smem));
     // the kernel moves registers between its warps: a build that is launched with fewer than it deals out would wait for ever
     cudaFuncAttributes fa;
     LOSA_CUDA_TRY(c, cudaFuncGetAttributes(&fa, kernel));
-    if (fa.numRegs < kWtLaunchRegs) return LOSA_ERR_UNSUPPORTED;
-    c->window_attr_set |= 1;
+    if (fa.numRegs < Tc::launch_regs) return LOSA_ERR_UNSUPPORTED;
+    c->window_attr_set |= bit;
   }
-  return with_plan<kWtRows, kWtKeys, D>(c, p, st, __nv_bfloat16{}, [&]() -> int32_t {
-    launch_k(kernel, p.n_ctas, kWtWarps * 32, wt_smem<D>(), st, mk, mv, p);
+  return with_plan<Tc::rows, kWtKeys, D>(c, p, st, __nv_bfloat16{}, [&]() -> int32_t {
+    launch_k(kernel, p.n_ctas, Tc::warps * 32, Tc::smem, st, mk, mv, p);
     return after_launch(c);
   });
 }
@@ -194,21 +200,20 @@ int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t
   p.status = status_ptr(c);
   p.scale_log2 = c->shape.sm_scale * kLog2e;
   p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
-  auto run = [&](auto f) {
-    constexpr int FMT = decltype(f)::value;
-    return c->shape.head_dim == 128 ? launch_rows<FMT, 128>(c, p, st) : launch_rows<FMT, 64>(c, p, st);
-  };
-  switch (row_format(c, kv)) {
-    case kRowsF32: return run(std::integral_constant<int, kRowsF32>{});
-    case kRowsBf16: {
-      auto with_page = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        return c->shape.page_size == 16 ? launch_tc<D, 16>(c, p, kv, st) : c->shape.page_size == 32 ? launch_tc<D, 32>(c, p, kv, st) : launch_tc<D, 64>(c, p, kv, st);
-      };
-      return c->shape.head_dim == 128 ? with_page(std::integral_constant<int, 128>{}) : with_page(std::integral_constant<int, 64>{});
+  auto run = [&](auto f, auto d) -> int32_t {
+    constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
+    if constexpr (FMT == kRowsF32) {
+      return launch_f32<D>(c, p, st);
+    } else {
+      return c->shape.page_size == 16 ? launch_tc<FMT, D, 16>(c, p, kv, st) : c->shape.page_size == 32 ? launch_tc<FMT, D, 32>(c, p, kv, st) : launch_tc<FMT, D, 64>(c, p, kv, st);
     }
-    case kRowsFp8: return run(std::integral_constant<int, kRowsFp8>{});
-    default: return run(std::integral_constant<int, kRowsInt4>{});
+  };
+  auto with_dim = [&](auto f) { return c->shape.head_dim == 128 ? run(f, std::integral_constant<int, 128>{}) : run(f, std::integral_constant<int, 64>{}); };
+  switch (row_format(c, kv)) {
+    case kRowsF32: return with_dim(std::integral_constant<int, kRowsF32>{});
+    case kRowsBf16: return with_dim(std::integral_constant<int, kRowsBf16>{});
+    case kRowsFp8: return with_dim(std::integral_constant<int, kRowsFp8>{});
+    default: return with_dim(std::integral_constant<int, kRowsInt4>{});
   }
 }
 

@@ -7,9 +7,9 @@
 constexpr int kWinRows = 64, kWinKeys = 64, kWinThreads = 128;
 template <int D> constexpr int win_smem() { return (kWinRows * D + kWinKeys * (D + 4) + kWinKeys * D + kWinRows * (kWinKeys + 4)) * 4; }
 
-template <int FMT, int D>
+template <int D>
 __global__ void __launch_bounds__(kWinThreads, 2) window_f32_kernel(const __grid_constant__ WindowParams p) {
-  using T = typename RowFormat<FMT>::Query;
+  using T = float;
   constexpr int R = kWinRows, GT = kWinKeys, KS = D + 4, PS = GT + 4, C8 = D / 8, NC = D / 64;
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sk = sq + R * D, *sv = sk + GT * KS, *sp = sv + GT * D;
@@ -57,8 +57,8 @@ __global__ void __launch_bounds__(kWinThreads, 2) window_f32_kernel(const __grid
         if (key < w.r.end && (key >= w.r.lo || key < p.q.sinks)) {
           const int page = page_of(p.c, w.s, key / p.c.g, p.status), slot = key % p.c.g;
           if (page >= 0) {
-            cache_load8<FMT, D>(p.c, p.c.k_pages, p.c.k_scale, page, w.kh, slot, ch, kx);
-            cache_load8<FMT, D>(p.c, p.c.v_pages, p.c.v_scale, page, w.kh, slot, ch, vx);
+            cache_load8<kRowsF32, D>(p.c, p.c.k_pages, p.c.k_scale, page, w.kh, slot, ch, kx);
+            cache_load8<kRowsF32, D>(p.c, p.c.v_pages, p.c.v_scale, page, w.kh, slot, ch, vx);
           }
         }
 #pragma unroll

@@ -13,16 +13,24 @@
 // Tensor memory is full: scores and output of either set, 128 columns each.  Everything is handed on by mbarriers with bounded waits.
 #pragma once
 
-constexpr int kWtRows = 256, kWtKeys = 128, kWtSoftWarps = 8;
-constexpr int kWtLoadWarp = 8, kWtQkWarp = 9, kWtPvWarp = 10, kWtFixWarp = 11, kWtWarps = 12;
-constexpr int kWtNK = 2, kWtNV = 3;
-// Registers per thread at the launch, and as they are dealt out: 8 x 32 x 208 + 4 x 32 x 80 <= 384 x 168
-constexpr int kWtLaunchRegs = 168, kWtSoftRegs = 208, kWtOtherRegs = 80;
-static_assert(kWtSoftWarps * kWtSoftRegs + (kWtWarps - kWtSoftWarps) * kWtOtherRegs <= kWtWarps * kWtLaunchRegs, "registers");
+constexpr int kWtKeys = 128, kWtSoftWarps = 8;
+constexpr int kWtLoadWarp = 8, kWtQkWarp = 9, kWtPvWarp = 10, kWtFixWarp = 11, kWtConvertWarp = 12;
 constexpr float kWtNone = -3.0e38f;                 // reference of a row that has seen no key
 constexpr float kWtTau = 8.f, kWtFused = 1048576.f;  // a reference up to this: its product with the scale may be subtracted in one operation
-template <int D> constexpr int wt_tile() { return kWtKeys * D * 2; }
-template <int D> constexpr int wt_smem() { return 1024 + 2 * 128 * D * 2 + (kWtNK + kWtNV) * wt_tile<D>() + 512; }
+// Quantised pages leave room for half the rows, and four more warps.
+template <int FMT, int D, int GP> struct WindowTc {
+  static constexpr bool quant = FMT != kRowsBf16;
+  static constexpr int rows = quant ? 128 : 256, warps = quant ? 16 : 12;
+  static constexpr int nk = 2, nv = quant ? 2 : 3, nr = 2;       // tiles of keys, of values; of either as they lie
+  // registers per thread at the launch, and as they are dealt out
+  static constexpr int launch_regs = quant ? 128 : 168, soft_regs = quant ? 184 : 208, other_regs = quant ? 72 : 80;
+  static_assert(kWtSoftWarps * soft_regs + (warps - kWtSoftWarps) * other_regs <= warps * launch_regs, "registers");
+  static constexpr int tile = kWtKeys * D * 2, qtile = 128 * D * 2;
+  static constexpr int raw = quant ? RawTile<FMT, D, GP>::bytes : 0;
+  static constexpr int tail = rows / 128 * qtile + (nk + nv) * tile + 2 * nr * raw;       // where the barriers lie
+  static constexpr int smem = 1024 + tail + 512;
+  static_assert(smem <= 232448, "shared memory");
+};
 
 __device__ __forceinline__ void wt_store16(void* at, bool on, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p st.global.v4.b32 [%0], {%2, %3, %4, %5};\n\t}"
@@ -43,35 +51,43 @@ __device__ __forceinline__ bool in_part(const WindowParams& p, const Common& c, 
   return key0 + kWtKeys > c.end || (key0 < c.lo && key0 + kWtKeys > p.q.sinks);
 }
 
-template <int D, int GP>
-__global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+template <int FMT, int D, int GP>
+__global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                     const __grid_constant__ WindowParams p) {
-  constexpr int R = kWtRows, GT = kWtKeys, TILE = wt_tile<D>(), HS = GT * 128, PG = GT / GP, QTILE = 128 * D * 2;
+  using Tc = WindowTc<FMT, D, GP>;
+  constexpr bool QUANT = Tc::quant;
+  constexpr int R = Tc::rows, GT = kWtKeys, TILE = Tc::tile, HS = GT * 128, PG = GT / GP, QTILE = Tc::qtile, TAIL = Tc::tail, QALL = R / 128 * QTILE;
+  constexpr int kWtNK = Tc::nk, kWtNV = Tc::nv, NR = Tc::nr;
   constexpr uint32_t COL_S = 0, COL_O = 256;         // tensor-memory columns: scores and outputs of the two sets, 128 each
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t qtile = base, kring = base + 2 * QTILE, vring = kring + kWtNK * TILE;
-  constexpr int TAIL = 2 * QTILE + (kWtNK + kWtNV) * TILE;
+  const uint32_t qtile = base, kring = base + QALL, vring = kring + kWtNK * TILE;
+  [[maybe_unused]] constexpr int RAW = QALL + (kWtNK + kWtNV) * TILE;       // quantised pages as they lie: [tensor][slot]
   const uint32_t bars = base + TAIL;
   const uint32_t k_full = bars, k_free = k_full + 8 * kWtNK, v_full = k_free + 8 * kWtNK, v_free = v_full + 8 * kWtNV, v_fixed = v_free + 8 * kWtNV;
   const uint32_t s_full = v_fixed + 8 * kWtNV, s_free = s_full + 16, p_full = s_free + 16, q_full = p_full + 32, o_free = q_full + 16, drain = o_free + 16;
-  static_assert(8 * (2 * kWtNK + 3 * kWtNV + 2 + 2 + 4 + 2 + 2 + 2) <= 256, "barriers");
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + TAIL + 256);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + TAIL + 260);
+  [[maybe_unused]] const uint32_t r_full = drain + 16, r_free = r_full + 16 * NR;       // [tensor][slot]
+  static_assert(8 * (2 * kWtNK + 3 * kWtNV + 2 + 2 + 4 + 2 + 2 + 2 + 4 * NR) <= 320, "barriers");
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + TAIL + 320);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + TAIL + 324);
   // [kOdd] the last piece (counting from one those that have groups) that has met what is no finite number.  The warp that looks is at most the V ring
   // ahead of the end of a piece, so a number is read before it is replaced.
   constexpr int kOdd = 8;
   static_assert(kOdd > kWtNV + 1, "pieces ahead");
-  volatile int* odd_piece = reinterpret_cast<volatile int*>(gen + TAIL + 264);
-  float* xm = reinterpret_cast<float*>(gen + QTILE);                   // [set][128] reference, sum: at the end of a piece that both sets have (the second tile of Q is not in use then)
+  volatile int* odd_piece = reinterpret_cast<volatile int*>(gen + TAIL + 328);
+  // [set][128] reference, sum: at the end of a piece that both sets have.  It lies in the second tile of Q, which is not in use then, or in the only one, once
+  // both sets' products have run.
+  float* xm = reinterpret_cast<float*>(gen + (QUANT ? 0 : QTILE));
   float* xl = xm + 256;
   const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
 
   grid_dep_trigger();                                // (the merging kernel comes up beside this one)
   if (tid == 0) {
-    for (int i = 0; i < kWtNK; ++i) { mbar_init(k_full + 8 * i, 1); mbar_init(k_free + 8 * i, 1); }
-    for (int i = 0; i < kWtNV; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_free + 8 * i, 1); mbar_init(v_fixed + 8 * i, 1); }
+    for (int i = 0; i < kWtNK; ++i) { mbar_init(k_full + 8 * i, QUANT ? 4 : 1); mbar_init(k_free + 8 * i, 1); }
+    if constexpr (QUANT)
+      for (int i = 0; i < 2 * NR; ++i) { mbar_init(r_full + 8 * i, 32); mbar_init(r_free + 8 * i, 4); }
+    for (int i = 0; i < kWtNV; ++i) { mbar_init(v_full + 8 * i, QUANT ? 4 : 1); mbar_init(v_free + 8 * i, 1); mbar_init(v_fixed + 8 * i, 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);                  // tcgen05.commit after Q K^T
       mbar_init(s_free + 8 * i, 1);                  // tcgen05.commit after P V: the scores may be replaced, the set's output holds them
@@ -110,7 +126,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
   __syncwarp();
   if (warp < kWtSoftWarps) {
     // ================================================================== softmax: thread = (set, row)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWtSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Tc::soft_regs));
     const int set = warp >> 2, at128 = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_at = tmem + COL_S + set * 128 + lanes, o_at = tmem + COL_O + set * 128 + lanes;
@@ -241,6 +257,11 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       float f0 = 1.f, f1 = 0.f, top = M, L = l;      // both sets: what either's output counts
       bool use0 = n > n0 && m != kWtNone, use1 = false;
       if (both) {
+        if constexpr (QUANT) {
+          tc5_fence_before();
+          all_meet();
+          tc5_fence_after();
+        }
         xm[set * 128 + at128] = M;
         xl[set * 128 + at128] = l;
         tc5_fence_before();
@@ -256,7 +277,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       }
       tc5_fence_after();
       const Piece following = next();
-      const bool q_now = !both || joint(following);      // (else the exchange lies where the second tile goes)
+      const bool q_now = !both || (!QUANT && joint(following));      // (else the exchange lies where the tile goes)
       if (q_now) write_q(following);
       if (filled(w)) ++pieces;
       const bool whole = w.whole(), odd = filled(w) && odd_piece[pieces % kOdd] == pieces;
@@ -292,7 +313,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                   float v[8];
-                  cache_load8<kRowsBf16, D>(p.c, p.c.v_pages, p.c.v_scale, page, w.kh, key % GP, c * 2 + h, v);
+                  cache_load8<FMT, D>(p.c, p.c.v_pages, p.c.v_scale, page, w.kh, key % GP, c * 2 + h, v);
 #pragma unroll
                   for (int k = 0; k < 8; ++k)
                     if (!(fabsf(v[k]) < INFINITY)) {
@@ -334,7 +355,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
       w = following;
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWtOtherRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Tc::other_regs));
     if (warp == kWtLoadWarp) {
       // ================================================================== pages
       int g = 0, nk = 0, nv = 0;                     // groups; copies begun
@@ -348,37 +369,48 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
             if (key < w.r.end && (key + GP > w.r.lo || key < p.q.sinks)) pages = max(0, page_of(p.c, w.s, key / GP, p.status));
             __syncwarp();
           }
-          const uint32_t have = __ballot_sync(0xffffffffu, pages >= 0) >> (i * PG) & ((1u << PG) - 1u);
-          const uint32_t bytes = __popc(have) * (GP * D * 2);
-          const int ks = g % kWtNK, vs = g % kWtNV;
-          if (g >= kWtNK && !wait(k_free + 8 * ks, (g / kWtNK - 1) & 1)) break;
-          if (elect_one()) mbar_expect_tx(k_full + 8 * ks, bytes);
-          ++nk;
-          __syncwarp();
-#pragma unroll 1
-          for (int j = 0; j < PG; ++j) {
-            const int page = __shfl_sync(0xffffffffu, pages, i * PG + j);
-            if (page >= 0 && elect_one())
-#pragma unroll
-              for (int h = 0; h < D / 64; ++h) tma_load_page(kring + ks * TILE + h * HS + j * GP * 128, &map_k, k_full + 8 * ks, h * 64, w.kh, page);
+          [[maybe_unused]] const uint32_t have = __ballot_sync(0xffffffffu, pages >= 0) >> (i * PG) & ((1u << PG) - 1u);
+          if constexpr (QUANT) {
+            const int slot = g % NR;
+            if (g >= NR && !wait(r_free + 8 * slot, (g / NR - 1) & 1)) break;
+            raw_load<FMT, D, GP>(p.c, p.c.k_pages, p.c.k_scale, w.kh, pages, i * PG, base + RAW + slot * Tc::raw, r_full + 8 * slot);
+            ++nk;
+            if (g >= NR && !wait(r_free + 8 * (NR + slot), (g / NR - 1) & 1)) break;
+            raw_load<FMT, D, GP>(p.c, p.c.v_pages, p.c.v_scale, w.kh, pages, i * PG, base + RAW + (NR + slot) * Tc::raw, r_full + 8 * (NR + slot));
+            ++nv;
+          } else {
+            const uint32_t bytes = __popc(have) * (GP * D * 2);
+            const int ks = g % kWtNK, vs = g % kWtNV;
+            if (g >= kWtNK && !wait(k_free + 8 * ks, (g / kWtNK - 1) & 1)) break;
+            if (elect_one()) mbar_expect_tx(k_full + 8 * ks, bytes);
+            ++nk;
             __syncwarp();
-          }
-          if (g >= kWtNV && !wait(v_free + 8 * vs, (g / kWtNV - 1) & 1)) break;
-          if (elect_one()) mbar_expect_tx(v_full + 8 * vs, bytes);
-          ++nv;
-          __syncwarp();
 #pragma unroll 1
-          for (int j = 0; j < PG; ++j) {
-            const int page = __shfl_sync(0xffffffffu, pages, i * PG + j);
-            if (page >= 0 && elect_one())
+            for (int j = 0; j < PG; ++j) {
+              const int page = __shfl_sync(0xffffffffu, pages, i * PG + j);
+              if (page >= 0 && elect_one())
 #pragma unroll
-              for (int h = 0; h < D / 64; ++h) tma_load_page(vring + vs * TILE + h * HS + j * GP * 128, &map_v, v_full + 8 * vs, h * 64, w.kh, page);
+                for (int h = 0; h < D / 64; ++h) tma_load_page(kring + ks * TILE + h * HS + j * GP * 128, &map_k, k_full + 8 * ks, h * 64, w.kh, page);
+              __syncwarp();
+            }
+            if (g >= kWtNV && !wait(v_free + 8 * vs, (g / kWtNV - 1) & 1)) break;
+            if (elect_one()) mbar_expect_tx(v_full + 8 * vs, bytes);
+            ++nv;
             __syncwarp();
+#pragma unroll 1
+            for (int j = 0; j < PG; ++j) {
+              const int page = __shfl_sync(0xffffffffu, pages, i * PG + j);
+              if (page >= 0 && elect_one())
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) tma_load_page(vring + vs * TILE + h * HS + j * GP * 128, &map_v, v_full + 8 * vs, h * 64, w.kh, page);
+              __syncwarp();
+            }
           }
         }
       }
       // (what is in flight has landed before the CTA's shared memory is given up)
-      if (!ok) {
+      if constexpr (QUANT) asm volatile("cp.async.wait_all;" ::: "memory");
+      else if (!ok) {
         for (int i = 0; i < min(kWtNK, nk); ++i) mbar_drain(k_full + 8 * i, ((nk - 1 - i) / kWtNK) & 1);
         for (int i = 0; i < min(kWtNV, nv); ++i) mbar_drain(v_full + 8 * i, ((nv - 1 - i) / kWtNV) & 1);
       }
@@ -453,7 +485,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
           }
         }
       }
-    } else {
+    } else if (warp == kWtFixWarp) {
       // ================================================================== values that must not count
       int g = 0, pieces = 0;
       for (Piece w = next(); w.any && ok; w = next()) {
@@ -463,7 +495,7 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
           const int key0 = group_key<GT>(w.r, gi), slot = g % kWtNV;
           if (!wait(v_full + 8 * slot, (g / kWtNV) & 1)) break;
           if (in_part(p, com, key0)) {
-            uint8_t* tile = gen + 2 * QTILE + (kWtNK + slot) * TILE;
+            uint8_t* tile = gen + QALL + (kWtNK + slot) * TILE;
             bool odd = false;
             // 16 bytes per lane, four 128-byte rows of the tile at a time
 #pragma unroll 2
@@ -496,6 +528,31 @@ __global__ void __launch_bounds__(kWtWarps * 32, 1) window_tc_kernel(const __gri
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(v_fixed + 8 * slot, 1);
+        }
+      }
+    } else {
+      // ================================================================== quantised pages into operands
+      if constexpr (QUANT) {
+        int g = 0;
+        for (Piece w = next(); w.any && ok; w = next()) {
+          for (int gi = w.first; gi < w.last && ok; ++gi, ++g) {
+#pragma unroll 1
+            for (int v = 0; v < 2; ++v) {
+              const int slot = g % NR, to = v ? g % kWtNV : g % kWtNK;
+              const uint32_t full = (v ? v_full : k_full) + 8 * to, free = (v ? v_free : k_free) + 8 * to;
+              const int turns = v ? g / kWtNV : g / kWtNK;
+              if (!wait(r_full + 8 * (v * NR + slot), (g / NR) & 1)) break;
+              if (turns > 0 && !wait(free, (turns - 1) & 1)) break;
+              raw_convert<FMT, D, GP>(gen + RAW + (v * NR + slot) * Tc::raw, gen + QALL + ((v ? kWtNK : 0) + to) * TILE, tid - kWtConvertWarp * 32);
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the products read the tile through the async proxy
+              __syncwarp();
+              if (lane == 0) {
+                mbar_arrive(full, 1);
+                mbar_arrive(r_free + 8 * (v * NR + slot), 1);
+              }
+              __syncwarp();
+            }
+          }
         }
       }
     }
