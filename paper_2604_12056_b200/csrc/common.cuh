@@ -61,6 +61,11 @@ struct losa_ctx {
   int64_t tmap_strides[3];
   int32_t tmap_n_phys;
   int32_t tmap_format;
+  // likewise of quantised pools as they lie, for the kernels that turn them into operands
+  alignas(64) unsigned char tmap_raw[2][128];
+  const void* tmap_raw_key[2];
+  int64_t tmap_raw_strides[3];
+  int32_t tmap_raw_n_phys, tmap_raw_format;
   void* encode_fn;  // cuTensorMapEncodeTiled, resolved through the runtime
   // second stream and fork/join events of the whole-step path (created on first use)
   cudaStream_t side_stream;

@@ -75,6 +75,8 @@ int32_t launch_sparse_prefix_attn(losa_ctx* c, const void* q, const losa_kv_t* k
 int32_t prepare_sparse_prefix_attn(losa_ctx* c, const losa_kv_t* kv);
 // Tensor maps of the pools (tmap_k, tmap_v of the context; bf16: boxes of a page's tokens by 64 elements, swizzled).
 int32_t pool_tensor_maps(losa_ctx* c, const losa_kv_t* kv);
+// Likewise of quantised pools (tmap_raw): boxes of a page's whole rows as they lie.
+int32_t raw_tensor_maps(losa_ctx* c, const losa_kv_t* kv);
 // Whole-step path: with defer_combine the main kernel leaves its partial records unmerged and
 // launch_attn_finish merges them, merges with the in-block part, writes the output, keeps the
 // queries and bumps the step (one kernel instead of two).

@@ -57,12 +57,10 @@ int32_t launch_f32(losa_ctx* c, const WeightParams& p, cudaStream_t st) {
 template <int FMT, int D, int GP>
 int32_t launch_tc(losa_ctx* c, WeightParams& p, const losa_kv_t* kv, cudaStream_t st) {
   using Tc = WeightsTc<FMT, D, GP>;
-  CUtensorMap mk = {};
-  if constexpr (!Tc::quant) {
-    const int32_t rc = pool_tensor_maps(c, kv);
-    if (rc != LOSA_OK) return rc;
-    memcpy(&mk, c->tmap_k, sizeof(mk));
-  }
+  const int32_t rc = Tc::quant ? raw_tensor_maps(c, kv) : pool_tensor_maps(c, kv);
+  if (rc != LOSA_OK) return rc;
+  CUtensorMap mk;
+  memcpy(&mk, Tc::quant ? c->tmap_raw[0] : c->tmap_k, sizeof(mk));
   p.n_ctas = c->n_sms;
   p.pad = 1;
   p.least = 2;

@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
   if (tid == 0) {
     for (int i = 0; i < NK; ++i) { mbar_init(k_full + 8 * i, QUANT ? 4 : 1); mbar_init(k_free + 8 * i, 1); }
     if constexpr (QUANT)
-      for (int i = 0; i < NR; ++i) { mbar_init(r_full + 8 * i, 32); mbar_init(r_free + 8 * i, 4); }
+      for (int i = 0; i < NR; ++i) { mbar_init(r_full + 8 * i, 1); mbar_init(r_free + 8 * i, 4); }
     for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, Tc::q_warps); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
     for (int i = 0; i < kKwBufs; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_free + 8 * i, 4); }
     mbar_init(drain, 1);
@@ -197,7 +197,10 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       __syncwarp();
       if constexpr (QUANT) {
         if (n >= NR && !wait(r_free + 8 * slot, (n / NR - 1) & 1)) break;
-        raw_load<FMT, D, GP>(p.c, p.c.k_pages, p.c.k_scale, w.kh, page, 0, base + RAW + slot * Tc::raw, r_full + 8 * slot);
+        float scale = 0.f;
+        if (FMT == kRowsFp8 && page >= 0) scale = static_cast<const float*>(p.c.k_scale)[static_cast<size_t>(page) * p.c.Hkv + w.kh];
+        __syncwarp();
+        raw_load<FMT, D, GP>(p.c, &map_k, p.c.k_scale, w.kh, page, scale, 0, base + RAW + slot * Tc::raw, r_full + 8 * slot);
         ++n;
         continue;
       }
@@ -216,9 +219,9 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       ++n;
     }
     // (what is in flight has landed before the CTA's shared memory is given up)
-    if constexpr (QUANT) asm volatile("cp.async.wait_all;" ::: "memory");
-    else if (!ok)
-      for (int i = 0; i < min(NK, n); ++i) mbar_drain(k_full + 8 * i, ((n - 1 - i) / NK) & 1);
+    constexpr int slots = QUANT ? NR : NK;
+    if (!ok)
+      for (int i = 0; i < min(slots, n); ++i) mbar_drain((QUANT ? r_full : k_full) + 8 * i, ((n - 1 - i) / slots) & 1);
     __syncwarp();
   } else if (warp == kKwMmaWarp) {
     // ================================================================== K Q^T
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
         const int slot = n % NR, to = n % NK;
         if (!wait(r_full + 8 * slot, (n / NR) & 1)) break;
         if (n >= NK && !wait(k_free + 8 * to, (n / NK - 1) & 1)) break;
-        raw_convert<FMT, D, GP>(gen + RAW + slot * Tc::raw, gen + to * TILE, tid - Tc::convert_warp * 32);
+        raw_convert<FMT, D, GP, false>(gen + RAW + slot * Tc::raw, gen + to * TILE, tid - Tc::convert_warp * 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the products read the tile through the async proxy
         __syncwarp();
         if (lane == 0) {

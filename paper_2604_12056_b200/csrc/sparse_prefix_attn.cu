@@ -418,15 +418,16 @@ int32_t encode_pool_map(losa_ctx* c, unsigned char* blob, const void* pool, cons
     if (!fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorSymbolNotFound);
     c->encode_fn = fn;
   }
-  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(sh.head_dim), static_cast<cuuint64_t>(sh.page_size),
+  const int row = kv->kv_format == LOSA_KV_INT4 ? sh.head_dim / 2 : sh.head_dim;
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(row), static_cast<cuuint64_t>(sh.page_size),
                               static_cast<cuuint64_t>(sh.n_kv_heads), static_cast<cuuint64_t>(kv->n_phys_pages)};
   // bf16 pages: 64-element (128-byte) boxes with the 128-byte swizzle, as the MMA descriptors expect them;
-  // FP8 pages: whole rows of d bytes; swizzled over the row (an MMA operand), or as they lie (V that the kernel converts)
-  const bool fp8 = kv->kv_format == LOSA_KV_FP8_E4M3;
+  // FP8 and 4-bit pages: whole rows of d or d / 2 bytes; swizzled over the row (an MMA operand), or as they lie (V that the kernel converts)
+  const bool fp8 = kv->kv_format != LOSA_KV_NATIVE;
   const cuuint64_t es = fp8 ? 1 : 2;
   const cuuint64_t strides[3] = {static_cast<cuuint64_t>(kv->stride_tok) * es, static_cast<cuuint64_t>(kv->stride_head) * es,
                                  static_cast<cuuint64_t>(kv->stride_page) * es};
-  const cuuint32_t box[4] = {fp8 ? static_cast<cuuint32_t>(sh.head_dim) : 64u, static_cast<cuuint32_t>(sh.page_size), 1, 1};
+  const cuuint32_t box[4] = {fp8 ? static_cast<cuuint32_t>(row) : 64u, static_cast<cuuint32_t>(sh.page_size), 1, 1};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUresult r = reinterpret_cast<EncodeTiledFn>(c->encode_fn)(
       reinterpret_cast<CUtensorMap*>(blob), fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
@@ -552,6 +553,26 @@ int32_t launch_f32(losa_ctx* c, const AttnParams& ap, cudaStream_t st, bool with
 
 
 int32_t pool_tensor_maps(losa_ctx* c, const losa_kv_t* kv) { return ensure_tensor_maps(c, kv); }
+int32_t raw_tensor_maps(losa_ctx* c, const losa_kv_t* kv) {
+  if (c->tmap_raw_key[0] == kv->k_pages && c->tmap_raw_key[1] == kv->v_pages && c->tmap_raw_strides[0] == kv->stride_page &&
+      c->tmap_raw_strides[1] == kv->stride_head && c->tmap_raw_strides[2] == kv->stride_tok && c->tmap_raw_n_phys == kv->n_phys_pages &&
+      c->tmap_raw_format == kv->kv_format)
+    return LOSA_OK;
+  alignas(64) unsigned char k[128], v[128];
+  int32_t rc = encode_pool_map(c, k, kv->k_pages, kv, true);
+  if (rc == LOSA_OK) rc = encode_pool_map(c, v, kv->v_pages, kv, true);
+  if (rc != LOSA_OK) return rc;
+  memcpy(c->tmap_raw[0], k, sizeof(k));
+  memcpy(c->tmap_raw[1], v, sizeof(v));
+  c->tmap_raw_key[0] = kv->k_pages;
+  c->tmap_raw_key[1] = kv->v_pages;
+  c->tmap_raw_strides[0] = kv->stride_page;
+  c->tmap_raw_strides[1] = kv->stride_head;
+  c->tmap_raw_strides[2] = kv->stride_tok;
+  c->tmap_raw_n_phys = kv->n_phys_pages;
+  c->tmap_raw_format = kv->kv_format;
+  return LOSA_OK;
+}
 
 int32_t prepare_sparse_prefix_attn(losa_ctx* c, const losa_kv_t* kv) {
   const bool bf = c->shape.dtype == LOSA_BF16, fp8 = kv->kv_format == LOSA_KV_FP8_E4M3;     // (FP8 pages: bf16 contexts only)

@@ -163,13 +163,11 @@ int32_t launch_f32(losa_ctx* c, WindowParams& p, cudaStream_t st) {
 template <int FMT, int D, int GP>
 int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_t st) {
   using Tc = WindowTc<FMT, D, GP>;
-  CUtensorMap mk = {}, mv = {};
-  if constexpr (!Tc::quant) {
-    const int32_t rc = pool_tensor_maps(c, kv);
-    if (rc != LOSA_OK) return rc;
-    memcpy(&mk, c->tmap_k, sizeof(mk));
-    memcpy(&mv, c->tmap_v, sizeof(mv));
-  }
+  const int32_t rc = Tc::quant ? raw_tensor_maps(c, kv) : pool_tensor_maps(c, kv);
+  if (rc != LOSA_OK) return rc;
+  CUtensorMap mk, mv;
+  memcpy(&mk, Tc::quant ? c->tmap_raw[0] : c->tmap_k, sizeof(mk));
+  memcpy(&mv, Tc::quant ? c->tmap_raw[1] : c->tmap_v, sizeof(mv));
   p.n_ctas = c->n_sms;
   p.pad = 2;
   p.least = 3;

@@ -28,7 +28,7 @@ template <int FMT, int D, int GP> struct WindowTc {
   static constexpr int tile = kWtKeys * D * 2, qtile = 128 * D * 2;
   static constexpr int raw = quant ? RawTile<FMT, D, GP>::bytes : 0;
   static constexpr int tail = rows / 128 * qtile + (nk + nv) * tile + 2 * nr * raw;       // where the barriers lie
-  static constexpr int smem = 1024 + tail + 512;
+  static constexpr int smem = 1024 + tail + 512 + (quant ? 512 : 0);
   static_assert(smem <= 232448, "shared memory");
 };
 
@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
   constexpr bool QUANT = Tc::quant;
   constexpr int R = Tc::rows, GT = kWtKeys, TILE = Tc::tile, HS = GT * 128, PG = GT / GP, QTILE = Tc::qtile, TAIL = Tc::tail, QALL = R / 128 * QTILE;
   constexpr int kWtNK = Tc::nk, kWtNV = Tc::nv, NR = Tc::nr;
+  constexpr uint32_t kType = QUANT ? 0u : 1u;        // operands: fp16, bf16
   constexpr uint32_t COL_S = 0, COL_O = 256;         // tensor-memory columns: scores and outputs of the two sets, 128 each
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -80,13 +81,14 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
   // both sets' products have run.
   float* xm = reinterpret_cast<float*>(gen + (QUANT ? 0 : QTILE));
   float* xl = xm + 256;
+  [[maybe_unused]] float* xs = reinterpret_cast<float*>(gen + TAIL + 512);       // [128] quantised pages: what a row's scores are multiplied by
   const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
 
   grid_dep_trigger();                                // (the merging kernel comes up beside this one)
   if (tid == 0) {
     for (int i = 0; i < kWtNK; ++i) { mbar_init(k_full + 8 * i, QUANT ? 4 : 1); mbar_init(k_free + 8 * i, 1); }
     if constexpr (QUANT)
-      for (int i = 0; i < 2 * NR; ++i) { mbar_init(r_full + 8 * i, 32); mbar_init(r_free + 8 * i, 4); }
+      for (int i = 0; i < 2 * NR; ++i) { mbar_init(r_full + 8 * i, 1); mbar_init(r_free + 8 * i, 4); }
     for (int i = 0; i < kWtNV; ++i) { mbar_init(v_full + 8 * i, QUANT ? 4 : 1); mbar_init(v_free + 8 * i, 1); mbar_init(v_fixed + 8 * i, 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + 8 * i, 1);                  // tcgen05.commit after Q K^T
@@ -134,6 +136,9 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       __syncwarp();
       asm volatile("bar.sync 1, %0;" ::"n"(kWtSoftWarps * 32) : "memory");
     };
+    // fp16 weights are taken times 2^7, so that they keep eleven bits down to 2^-21 of a row's largest and are within 2^-32 of it below
+    constexpr float kLift = QUANT ? 7.f : 0.f;
+    // ... and queries times a power of two of their row, whose largest element comes to 2^14 .. 2^15 (one below 2^-28 of that loses low bits)
     // this thread's row of Q into the set's tile
     auto write_q = [&](const Piece& w) {
       if (!w.any || !filled(w)) return;
@@ -143,10 +148,34 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       if (set * 128 + (warp & 3) * 32 < w.rows) {
         const int row = w.row0 + r, t = row / p.c.G;
         const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.q) + (static_cast<long long>(w.x.cu) + t) * p.q.stride + (w.kh * p.c.G + row - t * p.c.G) * D;
+        if constexpr (QUANT) {
+          uint4 v[D / 8];
+          float amax = 0.f;
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 v = r < w.rows ? *reinterpret_cast<const uint4*>(src + c * 8) : make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(gen + set * QTILE + (c >> 3) * HS + tc5_sw(at128, c & 7)) = v;
+          for (int c = 0; c < D / 8; ++c) v[c] = r < w.rows ? *reinterpret_cast<const uint4*>(src + c * 8) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            float x[8];
+            load8(reinterpret_cast<const __nv_bfloat16*>(&v[c]), x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(x[k]));
+          }
+          const int e = max(-100, min(127, static_cast<int>(__float_as_uint(amax) >> 23) - 127));
+          const float up = pow2f(14 - e);
+          xs[at128] = p.scale_log2 * pow2f(e - 14);
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            float x[8];
+            load8(reinterpret_cast<const __nv_bfloat16*>(&v[c]), x);
+            *reinterpret_cast<uint4*>(gen + (c >> 3) * HS + tc5_sw(at128, c & 7)) =
+                make_uint4(pack_f16(x[0] * up, x[1] * up), pack_f16(x[2] * up, x[3] * up), pack_f16(x[4] * up, x[5] * up), pack_f16(x[6] * up, x[7] * up));
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 v = r < w.rows ? *reinterpret_cast<const uint4*>(src + c * 8) : make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(gen + set * QTILE + (c >> 3) * HS + tc5_sw(at128, c & 7)) = v;
+          }
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -156,8 +185,8 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
     Piece w = next();
     write_q(w);
     int n = 0, pieces = 0;                           // jobs of this set before; pieces with groups so far
-    const float sc = p.scale_log2;
     while (w.any) {
+      float sc = p.scale_log2;
       const bool both = joint(w);
       const int r = (both ? 0 : set * 128) + at128;
       const bool idle = r - lane >= w.rows;          // none of the warp's rows exists
@@ -168,6 +197,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
         if (!wait(s_full + 8 * set, n & 1)) break;
         tc5_fence_after();
         if (!idle) {
+          if (QUANT && n == n0) sc = xs[at128];
           uint32_t x[128];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tc5_ld32_nowait(s_at + c * 32, x + c * 32);
@@ -210,14 +240,14 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
             l *= f;
             m = to;
           }
-          const float shift = m == kWtNone ? 0.f : -m * sc;
+          const float shift = m == kWtNone ? 0.f : kLift - m * sc;
           // a reference so large that only differences can be scaled: subtracted from the scores first (not an infinite one, whose row is lost)
           const bool apart = __any_sync(0xffffffffu, fabsf(shift) > kWtFused && fabsf(shift) < INFINITY);
           if (apart) {
 #pragma unroll
             for (int k = 0; k < 128; ++k) x[k] = __float_as_uint(score(k) - (m == kWtNone ? 0.f : m));
           }
-          const float2 scale = make_float2(sc, sc), sh = apart ? make_float2(0.f, 0.f) : make_float2(shift, shift);
+          const float2 scale = make_float2(sc, sc), sh = apart ? make_float2(kLift, kLift) : make_float2(shift, shift);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -228,7 +258,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
               e.x = ex2(e.x);
               e.y = ex2(e.y);
               sum[k & 1] = add2_f32(sum[k & 1], e);
-              h[k] = pack_b16(e.x, e.y);
+              h[k] = QUANT ? pack_f16(e.x, e.y) : pack_b16(e.x, e.y);
             }
             tc5_st16(s_at + c * 16, h);
             if (c & 1) {
@@ -253,7 +283,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       }
       // ---- end of the piece
       if (n > n0) wait(s_free + 8 * set, (n - 1) & 1);
-      const float M = m == kWtNone ? -INFINITY : m * sc;
+      const float M = m == kWtNone ? -INFINITY : m * sc - kLift;
       float f0 = 1.f, f1 = 0.f, top = M, L = l;      // both sets: what either's output counts
       bool use0 = n > n0 && m != kWtNone, use1 = false;
       if (both) {
@@ -361,22 +391,27 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       int g = 0, nk = 0, nv = 0;                     // groups; copies begun
       for (Piece w = next(); w.any && ok; w = next()) {
         int pages = 0;                               // of the next 32 / PG groups, one per lane; -1: nobody sees it
+        [[maybe_unused]] float k_scale = 0.f, v_scale = 0.f;                   // FP8: theirs
         for (int gi = w.first; gi < w.last; ++gi, ++g) {
           const int i = (gi - w.first) % (32 / PG);
           if (i == 0) {
             const int mine = gi + lane / PG, key = mine < w.last ? group_key<GT>(w.r, mine) + (lane % PG) * GP : w.r.end;
             pages = -1;
             if (key < w.r.end && (key + GP > w.r.lo || key < p.q.sinks)) pages = max(0, page_of(p.c, w.s, key / GP, p.status));
+            if (FMT == kRowsFp8 && pages >= 0) {
+              k_scale = static_cast<const float*>(p.c.k_scale)[static_cast<size_t>(pages) * p.c.Hkv + w.kh];
+              v_scale = static_cast<const float*>(p.c.v_scale)[static_cast<size_t>(pages) * p.c.Hkv + w.kh];
+            }
             __syncwarp();
           }
           [[maybe_unused]] const uint32_t have = __ballot_sync(0xffffffffu, pages >= 0) >> (i * PG) & ((1u << PG) - 1u);
           if constexpr (QUANT) {
             const int slot = g % NR;
             if (g >= NR && !wait(r_free + 8 * slot, (g / NR - 1) & 1)) break;
-            raw_load<FMT, D, GP>(p.c, p.c.k_pages, p.c.k_scale, w.kh, pages, i * PG, base + RAW + slot * Tc::raw, r_full + 8 * slot);
+            raw_load<FMT, D, GP>(p.c, &map_k, p.c.k_scale, w.kh, pages, k_scale, i * PG, base + RAW + slot * Tc::raw, r_full + 8 * slot);
             ++nk;
             if (g >= NR && !wait(r_free + 8 * (NR + slot), (g / NR - 1) & 1)) break;
-            raw_load<FMT, D, GP>(p.c, p.c.v_pages, p.c.v_scale, w.kh, pages, i * PG, base + RAW + (NR + slot) * Tc::raw, r_full + 8 * (NR + slot));
+            raw_load<FMT, D, GP>(p.c, &map_v, p.c.v_scale, w.kh, pages, v_scale, i * PG, base + RAW + (NR + slot) * Tc::raw, r_full + 8 * (NR + slot));
             ++nv;
           } else {
             const uint32_t bytes = __popc(have) * (GP * D * 2);
@@ -409,15 +444,15 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
         }
       }
       // (what is in flight has landed before the CTA's shared memory is given up)
-      if constexpr (QUANT) asm volatile("cp.async.wait_all;" ::: "memory");
-      else if (!ok) {
-        for (int i = 0; i < min(kWtNK, nk); ++i) mbar_drain(k_full + 8 * i, ((nk - 1 - i) / kWtNK) & 1);
-        for (int i = 0; i < min(kWtNV, nv); ++i) mbar_drain(v_full + 8 * i, ((nv - 1 - i) / kWtNV) & 1);
+      if (!ok) {
+        constexpr int sk = QUANT ? NR : kWtNK, sv = QUANT ? NR : kWtNV;
+        for (int i = 0; i < min(sk, nk); ++i) mbar_drain((QUANT ? r_full : k_full) + 8 * i, ((nk - 1 - i) / sk) & 1);
+        for (int i = 0; i < min(sv, nv); ++i) mbar_drain((QUANT ? r_full + 8 * NR : v_full) + 8 * i, ((nv - 1 - i) / sv) & 1);
       }
       __syncwarp();
     } else if (warp == kWtQkWarp) {
       // ================================================================== Q K^T
-      const uint32_t qt = warp_uniform(qtile), kr = warp_uniform(kring), idesc = tc5_idesc(128, GT, 0, 1u, 1u);
+      const uint32_t qt = warp_uniform(qtile), kr = warp_uniform(kring), idesc = tc5_idesc(128, GT, 0, kType, kType);
       int g = 0, n[2] = {0, 0}, q0 = 0, q1 = 0;
       for (Piece w = next(); w.any && ok; w = next()) {
         const bool both = joint(w);
@@ -449,7 +484,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       }
     } else if (warp == kWtPvWarp) {
       // ================================================================== P V
-      const uint32_t vr = warp_uniform(vring), idesc = tc5_idesc(128, D, 1, 1u, 1u);
+      const uint32_t vr = warp_uniform(vring), idesc = tc5_idesc(128, D, 1, kType, kType);
       int g = 0, n[2] = {0, 0}, piece = 0;
       for (Piece w = next(); w.any && ok; w = next()) {
         const bool both = joint(w);
@@ -513,8 +548,9 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
                   uint32_t u[4];
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {
-                    u[k] = (old[k] & 0x7f80u) == 0x7f80u ? old[k] & 0xffff0000u : old[k];
-                    u[k] = (u[k] & 0x7f800000u) == 0x7f800000u ? u[k] & 0x0000ffffu : u[k];
+                    constexpr uint32_t kExp = QUANT ? 0x7c00u : 0x7f80u;
+                    u[k] = (old[k] & kExp) == kExp ? old[k] & 0xffff0000u : old[k];
+                    u[k] = (u[k] & (kExp << 16)) == kExp << 16 ? u[k] & 0x0000ffffu : u[k];
                   }
                   if (u[0] != old[0] || u[1] != old[1] || u[2] != old[2] || u[3] != old[3]) {
                     *at = make_uint4(u[0], u[1], u[2], u[3]);
@@ -543,7 +579,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
               const int turns = v ? g / kWtNV : g / kWtNK;
               if (!wait(r_full + 8 * (v * NR + slot), (g / NR) & 1)) break;
               if (turns > 0 && !wait(free, (turns - 1) & 1)) break;
-              raw_convert<FMT, D, GP>(gen + RAW + (v * NR + slot) * Tc::raw, gen + QALL + ((v ? kWtNK : 0) + to) * TILE, tid - kWtConvertWarp * 32);
+              raw_convert<FMT, D, GP, true>(gen + RAW + (v * NR + slot) * Tc::raw, gen + QALL + ((v ? kWtNK : 0) + to) * TILE, tid - kWtConvertWarp * 32);
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the products read the tile through the async proxy
               __syncwarp();
               if (lane == 0) {
