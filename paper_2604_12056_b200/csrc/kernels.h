@@ -75,6 +75,8 @@ int32_t launch_sparse_prefix_attn(losa_ctx* c, const void* q, const losa_kv_t* k
 int32_t prepare_sparse_prefix_attn(losa_ctx* c, const losa_kv_t* kv);
 // Tensor maps of the pools (tmap_k, tmap_v of the context; bf16: boxes of a page's tokens by 64 elements, swizzled).
 int32_t pool_tensor_maps(losa_ctx* c, const losa_kv_t* kv);
+// A map (128 bytes, aligned to 64) of bf16 queries [tokens, H_q, d]: boxes of box_tokens tokens, the heads of a KV head, 64 elements, swizzled.
+int32_t query_tensor_map(losa_ctx* c, const void* q, int64_t stride, int32_t n_tokens, int32_t box_tokens, void* map);
 // Likewise of quantised pools (tmap_raw): boxes of a page's whole rows as they lie.
 int32_t raw_tensor_maps(losa_ctx* c, const losa_kv_t* kv);
 // Whole-step path: with defer_combine the main kernel leaves its partial records unmerged and
@@ -115,9 +117,9 @@ int32_t launch_int4_prefix_attn(losa_ctx* c, const void* q, const losa_kv_t* kv,
                                 const int32_t* union_pages, const int32_t* union_count, losa_state_t* state, cudaStream_t st);
 
 // New tokens over the cache, each over the keys it sees; what every key gets of them; the tokens of least weight leave.
-// The attention's list of work lies in the workspace: its rows per tile are kPlanRows at least, its CTAs at most kPlanShares per SM, and
+// The attention's list of work lies in the workspace: its rows per tile are kPlanRows at least (whole tokens of a tile of 64), its CTAs at most kPlanShares per SM, and
 // they leave records of at most kPlanRecordRows rows per SM.
-constexpr int kPlanRows = 64, kPlanShares = 4, kPlanRecordRows = 512;
+constexpr int kPlanRows = 48, kPlanShares = 4, kPlanRecordRows = 512;
 int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t* kv, void* out, float* lse_opt, cudaStream_t st);
 int32_t launch_kv_weights(losa_ctx* c, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, cudaStream_t st);
 int32_t launch_kv_evict(losa_ctx* c, losa_kv_t* kv, float* weights, const losa_eviction_t* ev, cudaStream_t st);

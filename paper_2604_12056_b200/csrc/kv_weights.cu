@@ -20,21 +20,33 @@ struct WeightParams : ListParams {
   float scale_log2;
 };
 
-// Rows of a sequence that see any of the keys key0 .. key0 + n - 1.
-__device__ __forceinline__ int2 rows_over(const ListParams& p, const Sequence& x, int key0, int n) {
+// Tokens of a sequence that see any of the keys key0 .. key0 + n - 1: x .. y - 1.
+__device__ __forceinline__ int2 tokens_over(const ListParams& p, const Sequence& x, int key0, int n) {
   const int first = p.q.span == 1 ? key0 : key0 / p.q.span * p.q.span;              // the first place that sees key0
   const long long last = p.q.window == 0 || key0 < p.q.sinks ? 1ll << 40 : static_cast<long long>(key0) + n - 1 + p.q.window;
   const int t0 = min(max(0, first - x.start), x.count), t1 = static_cast<int>(max(0ll, min(static_cast<long long>(x.count), last - x.start)));
-  return make_int2(t0 * p.c.G, max(t0, t1) * p.c.G);
+  return make_int2(t0, max(t0, t1));
 }
 
-// A key's weight from the rows' sum.
-__device__ __forceinline__ void put_weight(const WeightParams& p, const Sequence& x, int s, int kh, int key, float sum) {
+// Where a key's weight stands (null: there is no such key), and what is left of it.
+struct Held {
+  float* at;
+  float old;
+  bool kept;
+};
+__device__ __forceinline__ Held held_weight(const WeightParams& p, const Sequence& x, int s, int kh, int key) {
+  Held h = {nullptr, 0.f, false};
+  if (key >= x.len) return h;
   const int page = page_of(p.c, s, key / p.c.g, p.status);
-  if (page < 0) return;
-  float* at = p.weights + (static_cast<size_t>(page) * p.c.Hkv + kh) * p.c.g + key % p.c.g;
-  // (what stood for tokens that are new is not looked at; with keep 0 neither is the rest)
-  *at = key < x.start && p.keep != 0.f ? fmaf(p.keep, *at, sum) : sum;
+  if (page < 0) return h;
+  h.at = p.weights + (static_cast<size_t>(page) * p.c.Hkv + kh) * p.c.g + key % p.c.g;
+  h.kept = key < x.start && p.keep != 0.f;           // (what stood for tokens that are new is not looked at; with keep 0 neither is the rest)
+  if (h.kept) h.old = *h.at;
+  return h;
+}
+// ... and the weight from the rows' sum.
+__device__ __forceinline__ void put_weight(const WeightParams& p, const Held& h, float sum) {
+  if (h.at) *h.at = h.kept ? fmaf(p.keep, h.old, sum) : sum;
 }
 
 #include "kv_weights_f32.cuh"
@@ -59,8 +71,14 @@ int32_t launch_tc(losa_ctx* c, WeightParams& p, const losa_kv_t* kv, cudaStream_
   using Tc = WeightsTc<FMT, D, GP>;
   const int32_t rc = Tc::quant ? raw_tensor_maps(c, kv) : pool_tensor_maps(c, kv);
   if (rc != LOSA_OK) return rc;
-  CUtensorMap mk;
+  CUtensorMap mk, mq;
   memcpy(&mk, Tc::quant ? c->tmap_raw[0] : c->tmap_k, sizeof(mk));
+  if (p.q.T > 0) {
+    const int32_t rq = query_tensor_map(c, p.q.q, p.q.stride, p.q.T, 128 / p.c.G, &mq);
+    if (rq != LOSA_OK) return rq;
+  } else {
+    mq = mk;                                         // (not used)
+  }
   p.n_ctas = c->n_sms;
   p.pad = 1;
   p.least = 2;
@@ -73,7 +91,7 @@ int32_t launch_tc(losa_ctx* c, WeightParams& p, const losa_kv_t* kv, cudaStream_
     c->window_attr_set |= bit;
   }
   launch_k(list_plan_kernel<KeyTiles>, 1, kPlanThreads, 0, st, static_cast<const ListParams&>(p));
-  launch_k(kernel, p.n_ctas, kKwWarps * 32, Tc::smem, st, mk, p);
+  launch_k(kernel, p.n_ctas, Tc::warps * 32, Tc::smem, st, mk, mq, p);
   launch_k(weights_join_kernel, p.n_ctas, kKwKeys, 0, st, p);
   return after_launch(c, 3);
 }

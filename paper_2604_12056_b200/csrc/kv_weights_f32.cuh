@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(kWgtThreads, 3) weights_f32_kernel(const __gri
   const int s = blockIdx.z, kh = blockIdx.y, key0 = blockIdx.x * GT;
   const Sequence x = sequence_of(p.c, p.q, s, blockIdx.x == 0 && kh == 0 && tid == 0 ? p.status : nullptr);
   if (key0 >= x.len) return;
-  const int2 rows = rows_over(p, x, key0, min(GT, x.len - key0));
+  const int2 seen = tokens_over(p, x, key0, min(GT, x.len - key0)), rows = make_int2(seen.x * p.c.G, seen.y * p.c.G);
   if (rows.x >= rows.y && p.keep == 1.f && key0 + GT <= x.start) return;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   if (rows.x < rows.y) {
@@ -90,6 +90,6 @@ __global__ void __launch_bounds__(kWgtThreads, 3) weights_f32_kernel(const __gri
     float total = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) total += part[i * GT + tid];
-    put_weight(p, x, s, kh, key0 + tid, total);
+    put_weight(p, held_weight(p, x, s, kh, key0 + tid), total);
   }
 }

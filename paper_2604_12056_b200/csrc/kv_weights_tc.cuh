@@ -3,18 +3,19 @@
 // Keys take the 128 lanes, query rows the columns, so that a thread has a key to itself and its sum never leaves the register: a job is
 // 128 keys by up to 128 rows.
 //   a warp            pages of keys by TMA into a ring of swizzled tiles
-//   three warps       rows of Q, and their log-normalisers, into another
+//   some warps        jobs by turns: queries by TMA, as many whole tokens as 128 rows hold, and their log-normalisers, into another
 //   S[128 x rows] = K Q^T   an issuing warp; four score tiles in tensor memory
 //   two sets of four warps  take alternate jobs: exponentials, added up by key; at a tile's end the sets' sums meet in shared memory
 // A key is seen by a run of rows, so a job that is not seen whole is masked by two numbers per thread.
 #pragma once
 
 constexpr int kKwKeys = 128, kKwRows = 128, kKwBufs = 4;
-constexpr int kKwSumWarps = 8, kKwLoadWarp = 8, kKwMmaWarp = 9, kKwQWarp = 10, kKwWarps = 16;
+constexpr int kKwSumWarps = 8, kKwLoadWarp = 8, kKwMmaWarp = 9, kKwQWarp = 10;
 template <int FMT, int D, int GP> struct WeightsTc {
   static constexpr bool quant = FMT != kRowsBf16;
-  static constexpr int q_warps = quant ? 2 : 6, convert_warp = kKwQWarp + q_warps;       // quantised pages: the last four warps turn them into operands
-  static constexpr int nk = quant ? 2 : 3, nq = 3, nr = 3;       // tiles of keys, of rows; of keys as they lie
+  static constexpr int q_warps = quant ? 2 : 3, convert_warp = kKwQWarp + 2;              // quantised pages: the last four warps turn them into operands
+  static constexpr int warps = quant ? 16 : 13;
+  static constexpr int nk = quant ? 2 : 3, nq = q_warps, nr = 3; // tiles of keys, of rows (one per warp that fills them: it waits for every one of its phases in turn); of keys as they lie
   static constexpr int tile = 128 * D * 2, raw = quant ? RawTile<FMT, D, GP>::bytes : 0;
   static constexpr int norms = (nk + nq) * tile + (quant ? nr * raw : 0), other = norms + nq * kKwRows * 4, tail = other + 2 * kKwKeys * 4;
   static constexpr int smem = 1024 + tail + 256;
@@ -41,25 +42,27 @@ struct KeyTiles {
   static __device__ __forceinline__ int tiles(const ListParams& p, const Sequence& x) { return key_reach(p, x).tiles; }
   static __device__ __forceinline__ int groups(const ListParams& p, const Sequence& x, int j) {
     const int key0 = tile_key(key_reach(p, x), j);
-    const int2 rows = rows_over(p, x, key0, min(kKwKeys, x.len - key0));
-    return (rows.y - rows.x + kKwRows - 1) / kKwRows;
+    const int2 seen = tokens_over(p, x, key0, min(kKwKeys, x.len - key0));
+    const int per = kKwRows / p.c.G;
+    return (seen.y - seen.x + per - 1) / per;
   }
 };
-struct KeyPiece : Part { int key0, row0, rows; };    // rows row0 .. row0 + rows - 1 see any of the tile's keys
+struct KeyPiece : Part { int key0, token0, tokens; };      // tokens token0 .. token0 + tokens - 1 see any of the tile's keys
 __device__ __forceinline__ KeyPiece next_keys(Walk& walk) {
   KeyPiece w;
   static_cast<Part&>(w) = walk.next();
   if (w.any) {
     w.key0 = tile_key(key_reach(walk.p, w.x), w.j);
-    const int2 rows = rows_over(walk.p, w.x, w.key0, min(kKwKeys, w.x.len - w.key0));
-    w.row0 = rows.x;
-    w.rows = rows.y - rows.x;
+    const int2 seen = tokens_over(walk.p, w.x, w.key0, min(kKwKeys, w.x.len - w.key0));
+    w.token0 = seen.x;
+    w.tokens = seen.y - seen.x;
   }
   return w;
 }
 
 template <int FMT, int D, int GP>
-__global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ WeightParams p) {
+__global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+                                                                     const __grid_constant__ WeightParams p) {
   using Tc = WeightsTc<FMT, D, GP>;
   constexpr bool QUANT = Tc::quant;
   constexpr int TILE = Tc::tile, HS = 128 * 128, PG = kKwKeys / GP, NK = Tc::nk, NQ = Tc::nq, NR = Tc::nr;
@@ -85,7 +88,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
     for (int i = 0; i < NK; ++i) { mbar_init(k_full + 8 * i, QUANT ? 4 : 1); mbar_init(k_free + 8 * i, 1); }
     if constexpr (QUANT)
       for (int i = 0; i < NR; ++i) { mbar_init(r_full + 8 * i, 1); mbar_init(r_free + 8 * i, 4); }
-    for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, Tc::q_warps); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
+    for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, 1); mbar_init(q_free + 8 * i, 1 + 4); }      // the products, and the set that reads the log-normalisers
     for (int i = 0; i < kKwBufs; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_free + 8 * i, 4); }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -112,6 +115,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
     return ok;
   };
   Walk walk(p, blockIdx.x);
+  const int per = kKwRows / p.c.G;                   // tokens of a job
   __syncwarp();
   if (warp < kKwSumWarps) {
     // ================================================================== sums: thread = (set, key)
@@ -121,15 +125,16 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
     int job = 0, turn = 0;
     for (KeyPiece w = next_keys(walk); w.any; w = next_keys(walk)) {
       const int key = w.key0 + at128, jobs = w.last - w.first;
-      // the rows, counted from the piece's first, that see this key
-      const int2 seen = rows_over(p, w.x, key, 1);
-      const int ra = seen.x - w.row0, rb = min(seen.y - w.row0, w.rows);
+      // the tokens, counted from the tile's first, that see this key
+      const int2 seen = tokens_over(p, w.x, key, 1);
+      const int ta = seen.x - w.token0, tb = min(seen.y - w.token0, w.tokens);
+      const Held held = held_weight(p, w.x, w.s, w.kh, key);             // (asked for before the sum)
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
         if ((job & 1) != set) continue;
-        const int buf = job % kKwBufs, slot = job % NQ, n = min(kKwRows, w.rows - gi * kKwRows);
-        const int a = ra - gi * kKwRows, b = rb - gi * kKwRows;          // of the job's columns this key counts a .. b - 1
-        const bool part = __any_sync(0xffffffffu, a > 0 || b < n);
+        const int buf = job % kKwBufs, slot = job % NQ, n = min(per, w.tokens - gi * per) * p.c.G;
+        const int a = (ta - gi * per) * p.c.G, b = min((tb - gi * per) * p.c.G, n);      // of the job's columns this key counts a .. b - 1
+        const bool part = __any_sync(0xffffffffu, a > 0 || b < n || (n & 31));      // (columns behind n may hold anything)
         if (!wait(s_full + 8 * buf, (job / kKwBufs) & 1)) break;
         tc5_fence_after();
         const float* norm = norms + slot * kKwRows;
@@ -179,7 +184,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       }
       if (set == writer && ok) {
         if (w.whole()) {
-          if (key < w.x.len) put_weight(p, w.x, w.s, w.kh, key, total);
+          put_weight(p, held, total);
         } else {
           p.partials[record_at(blockIdx.x, w.first == 0) * kKwKeys + at128] = total;
         }
@@ -208,14 +213,10 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       if (n >= NK && !wait(k_free + 8 * slot, (n / NK - 1) & 1)) break;
       if (elect_one()) mbar_expect_tx(k_full + 8 * slot, __popc(have) * (GP * D * 2));
       __syncwarp();
-#pragma unroll 1
-      for (int j = 0; j < PG; ++j) {
-        const int from = __shfl_sync(0xffffffffu, page, j);
-        if (from >= 0 && elect_one())
+      if (page >= 0)                                 // (each lane its page: a copy in a loop of the warp takes 185 cycles)
 #pragma unroll
-          for (int h = 0; h < D / 64; ++h) tma_load_page(kring + slot * TILE + h * HS + j * GP * 128, &map_k, k_full + 8 * slot, h * 64, w.kh, from);
-        __syncwarp();
-      }
+        for (int h = 0; h < D / 64; ++h) tma_load_page(kring + slot * TILE + h * HS + lane * GP * 128, &map_k, k_full + 8 * slot, h * 64, w.kh, page);
+      __syncwarp();
       ++n;
     }
     // (what is in flight has landed before the CTA's shared memory is given up)
@@ -231,8 +232,10 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       if (w.last == w.first) continue;
       const int kslot = n % NK;
       if (!wait(k_full + 8 * kslot, (n / NK) & 1)) break;
-      for (int gi = w.first; gi < w.last; ++gi, ++job) {
-        const int buf = job % kKwBufs, slot = job % NQ, cols = min(kKwRows, w.rows - gi * kKwRows);
+      // (numbers that the compiler knows to be the warp's: a product whose operands come from ordinary registers takes 120 cycles to issue)
+      const int first = warp_uniform(w.first), last = warp_uniform(w.last), tokens = warp_uniform(w.tokens);
+      for (int gi = first; gi < last; ++gi, ++job) {
+        const int buf = job % kKwBufs, slot = job % NQ, cols = min(per, tokens - gi * per) * p.c.G;
         if (!wait(q_full + 8 * slot, (job / NQ) & 1)) break;
         if (job >= kKwBufs && !wait(s_free + 8 * buf, (job / kKwBufs - 1) & 1)) break;
         tc5_fence_after();
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
           }
           tc5_commit(s_full + 8 * buf);
           tc5_commit(q_free + 8 * slot);
-          if (gi + 1 == w.last) tc5_commit(k_free + 8 * kslot);
+          if (gi + 1 == last) tc5_commit(k_free + 8 * kslot);
         }
         __syncwarp();
       }
@@ -279,43 +282,39 @@ __global__ void __launch_bounds__(kKwWarps * 32, 1) weights_tc_kernel(const __gr
       }
     }
   } else {
-    // ================================================================== rows of Q, sixteen (or eight) lanes to a row
-    constexpr int LPR = D / 8, RPW = 32 / LPR;       // lanes of 16 bytes per row, rows a warp takes at a time
-    const int qw = warp - kKwQWarp, col = lane % LPR, sub = lane / LPR;
-    auto landed = [&](int j, auto still) {           // (one job's copies stay in flight while the next one's are begun)
-      asm volatile("cp.async.wait_group %0;" ::"n"(decltype(still)::value) : "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // the products read the tile through the async proxy
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_full + 8 * (j % NQ), 1);
-      __syncwarp();
-    };
-    int job = 0;
+    // ================================================================== queries and log-normalisers, jobs by turns
+    const int mine = warp - kKwQWarp;
+    int tok[4], head[4];                             // of rows lane, lane + 32, ..
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      tok[i] = (lane + 32 * i) / p.c.G;
+      head[i] = lane + 32 * i - tok[i] * p.c.G;
+    }
+    int job = 0, begun = -1;                         // the last of this warp's jobs
     for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
-        const int slot = job % NQ, n = min(kKwRows, w.rows - gi * kKwRows), padded = (n + 31) & ~31;
+        if (job % Tc::q_warps != mine) continue;
+        const int slot = job % NQ, n = min(per, w.tokens - gi * per);
+        const long long t0 = static_cast<long long>(w.x.cu) + w.token0 + gi * per;
+        float l[4];                                  // a row that does not exist, or saw nothing, gives nothing
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] = tok[i] < n ? p.lse[(t0 + tok[i]) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + head[i]] : -INFINITY;
         if (job >= NQ && !wait(q_free + 8 * slot, (job / NQ - 1) & 1)) break;
-        uint8_t* tile = gen + (NK + slot) * TILE;
-        const int row0 = w.row0 + gi * kKwRows;
-        for (int i = qw * 32 + lane; i < padded; i += Tc::q_warps * 32) {
-          float l = INFINITY;                        // a row that does not exist, or saw nothing, gives nothing
-          if (i < n) {
-            const int t = (row0 + i) / p.c.G;
-            const float v = p.lse[(static_cast<long long>(w.x.cu) + t) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + (row0 + i - t * p.c.G)];
-            l = v == -INFINITY ? INFINITY : v * kLog2e;
-          }
-          norms[slot * kKwRows + i] = l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) norms[slot * kKwRows + lane + 32 * i] = l[i] == -INFINITY ? INFINITY : l[i] * kLog2e;
+        __syncwarp();
+        if (elect_one()) {
+          mbar_expect_tx(q_full + 8 * slot, per * p.c.G * D * 2);
+#pragma unroll
+          for (int h = 0; h < D / 64; ++h) tma_load_queries(qring + slot * TILE + h * HS, &map_q, q_full + 8 * slot, h * 64, w.kh * p.c.G, static_cast<int>(t0));
         }
-        for (int i = qw * RPW + sub; i < padded; i += Tc::q_warps * RPW) {
-          uint32_t dst = smem_u32(tile + (col >> 3) * HS + tc5_sw(i, col & 7));
-          const int r = i < n ? row0 + i : row0, t = r / p.c.G;
-          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.q) + (static_cast<long long>(w.x.cu) + t) * p.q.stride + (w.kh * p.c.G + r - t * p.c.G) * D + col * 8;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(i < n ? 16 : 0) : "memory");
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        if (job > 0) landed(job - 1, std::integral_constant<int, 1>{});
+        __syncwarp();
+        begun = job;
       }
     }
-    if (job > 0) landed(job - 1, std::integral_constant<int, 0>{});
+    // (what is in flight has landed before the CTA's shared memory is given up)
+    if (!ok && begun >= 0) mbar_drain(q_full + 8 * (begun % NQ), (begun / NQ) & 1);
+    __syncwarp();
   }
   tc5_fence_before();
   __syncthreads();
@@ -330,7 +329,8 @@ __global__ void __launch_bounds__(kKwKeys) weights_join_kernel(const __grid_cons
   const int last = records_from(p, b, x);
   if (last < b) return;
   const int key = tile_key(key_reach(p, x.t.x), x.t.j) + threadIdx.x;
+  const Held held = held_weight(p, x.t.x, x.t.s, x.kh, key);
   float total = 0.f;
   for (int i = b - 1; i <= last; ++i) total += p.partials[record_at(i, i == b - 1) * kKwKeys + threadIdx.x];
-  if (key < x.t.x.len) put_weight(p, x.t.x, x.t.s, x.kh, key, total);
+  put_weight(p, held, total);
 }

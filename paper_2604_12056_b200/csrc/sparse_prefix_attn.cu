@@ -409,15 +409,20 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
+int32_t find_encoder(losa_ctx* c) {
+  if (c->encode_fn) return LOSA_OK;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  LOSA_CUDA_TRY(c, cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+  if (!fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorSymbolNotFound);
+  c->encode_fn = fn;
+  return LOSA_OK;
+}
+
 int32_t encode_pool_map(losa_ctx* c, unsigned char* blob, const void* pool, const losa_kv_t* kv, bool plain) {
   const losa_shape_t& sh = c->shape;
-  if (!c->encode_fn) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    LOSA_CUDA_TRY(c, cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
-    if (!fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorSymbolNotFound);
-    c->encode_fn = fn;
-  }
+  const int32_t rc = find_encoder(c);
+  if (rc != LOSA_OK) return rc;
   const int row = kv->kv_format == LOSA_KV_INT4 ? sh.head_dim / 2 : sh.head_dim;
   const cuuint64_t dims[4] = {static_cast<cuuint64_t>(row), static_cast<cuuint64_t>(sh.page_size),
                               static_cast<cuuint64_t>(sh.n_kv_heads), static_cast<cuuint64_t>(kv->n_phys_pages)};
@@ -552,6 +557,21 @@ int32_t launch_f32(losa_ctx* c, const AttnParams& ap, cudaStream_t st, bool with
 }  // namespace
 
 
+int32_t query_tensor_map(losa_ctx* c, const void* q, int64_t stride, int32_t n_tokens, int32_t box_tokens, void* map) {
+  const losa_shape_t& sh = c->shape;
+  const int32_t rc = find_encoder(c);
+  if (rc != LOSA_OK) return rc;
+  const int G = sh.n_q_heads / sh.n_kv_heads;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(sh.head_dim), static_cast<cuuint64_t>(sh.n_q_heads), static_cast<cuuint64_t>(n_tokens)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(sh.head_dim) * 2, static_cast<cuuint64_t>(n_tokens > 1 ? stride : sh.n_q_heads * sh.head_dim) * 2};
+  const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(box_tokens)}, estr[3] = {1, 1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(c->encode_fn)(
+      static_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) return LOSA_OK;
+  c->last_cuda_error = static_cast<int32_t>(r);
+  return LOSA_ERR_CUDA;
+}
 int32_t pool_tensor_maps(losa_ctx* c, const losa_kv_t* kv) { return ensure_tensor_maps(c, kv); }
 int32_t raw_tensor_maps(losa_ctx* c, const losa_kv_t* kv) {
   if (c->tmap_raw_key[0] == kv->k_pages && c->tmap_raw_key[1] == kv->v_pages && c->tmap_raw_strides[0] == kv->stride_page &&

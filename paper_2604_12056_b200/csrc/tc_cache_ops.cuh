@@ -13,6 +13,11 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(0), "r"(head), "r"(page) : "memory");
 }
+// a box of queries: the heads of a KV head of consecutive tokens, 64 elements of each
+__device__ __forceinline__ void tma_load_queries(uint32_t dst, const CUtensorMap* map, uint32_t bar, int col, int head, int token) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(head), "r"(token) : "memory");
+}
 // two at a time
 __device__ __forceinline__ float max3_f32(float a, float b, float c) {
   float d;
@@ -58,17 +63,14 @@ __device__ __forceinline__ void raw_load(const CacheParams& c, const CUtensorMap
   }
   if (elect_one()) mbar_expect_tx(bar, __popc(have) * (GP * Raw::row + (FMT == kRowsInt4 ? kScaleBytes : 0)));
   __syncwarp();
-#pragma unroll 1
-  for (int j = 0; j < Raw::pages; ++j) {
-    const int page = __shfl_sync(0xffffffffu, pages, first + j);
-    if (page >= 0 && elect_one()) {
-      tma_load_page(dst + j * GP * Raw::row, map, bar, 0, kh, page);
-      if constexpr (FMT == kRowsInt4)
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + Raw::codes + j * kScaleBytes),
-                     "l"(static_cast<const uint8_t*>(scales) + (static_cast<size_t>(page) * c.Hkv + kh) * kScaleBytes), "r"(kScaleBytes), "r"(bar) : "memory");
-    }
-    __syncwarp();
+  const int j = lane - first;
+  if (j >= 0 && j < Raw::pages && pages >= 0) {
+    tma_load_page(dst + j * GP * Raw::row, map, bar, 0, kh, pages);
+    if constexpr (FMT == kRowsInt4)
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + Raw::codes + j * kScaleBytes),
+                   "l"(static_cast<const uint8_t*>(scales) + (static_cast<size_t>(pages) * c.Hkv + kh) * kScaleBytes), "r"(kScaleBytes), "r"(bar) : "memory");
   }
+  __syncwarp();
 }
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -107,7 +109,7 @@ template <int FMT, int D, int GP, bool HALF>
 __device__ __forceinline__ void raw_convert(const uint8_t* raw, uint8_t* tile, int id) {
   using Raw = RawTile<FMT, D, GP>;
   constexpr int E = 128 / RowFormat<FMT>::bits;      // elements of a piece
-#pragma unroll 4
+#pragma unroll 2
   for (int i = id; i < 128 * Raw::pieces; i += 128) {
     const int t = i / Raw::pieces, piece = i % Raw::pieces;
     const uint4 u = *reinterpret_cast<const uint4*>(raw + i * 16);

@@ -21,13 +21,12 @@ struct WindowParams : ListParams {
   float scale_log2;                                  // sm_scale * log2(e)
 };
 
-// The groups (of GT keys) that rows row0 .. of a sequence see: the first `first`, then those from `from` on, up to `end` keys.
+// The groups (of GT keys) that tokens t0 .. t0 + n - 1 of a sequence see: the first `first`, then those from `from` on, up to `end` keys.
 struct Reach { int first, from, groups, end, lo; };
 template <int GT>
-__device__ __forceinline__ Reach reach_of(const ListParams& p, const Sequence& x, int row0, int rows) {
-  const int t0 = row0 / p.c.G, t1 = min(x.count - 1, (row0 + rows - 1) / p.c.G);
+__device__ __forceinline__ Reach reach_of(const ListParams& p, const Sequence& x, int t0, int n) {
   Reach r;
-  r.end = keys_of(p.q, x, x.start + t1).x;
+  r.end = keys_of(p.q, x, x.start + t0 + n - 1).x;
   r.lo = keys_of(p.q, x, x.start + t0).y;
   const int sinks = r.lo > 0 ? min(p.q.sinks, r.end) : 0;
   r.first = (sinks + GT - 1) / GT;
@@ -37,48 +36,60 @@ __device__ __forceinline__ Reach reach_of(const ListParams& p, const Sequence& x
 }
 template <int GT> __device__ __forceinline__ int group_key(const Reach& r, int i) { return (i < r.first ? i : r.from + i - r.first) * GT; }
 
-template <int R, int GT>
+// A tile's rows: SETS sets of SR, each of as many whole tokens as fit.
+template <int SR, int SETS, int GT>
 struct RowTiles {
-  static __device__ __forceinline__ int tiles(const ListParams& p, const Sequence& x) { return static_cast<int>((static_cast<long long>(x.count) * p.c.G + R - 1) / R); }
-  static __device__ __forceinline__ int groups(const ListParams& p, const Sequence& x, int j) { return reach_of<GT>(p, x, j * R, R).groups; }
+  static constexpr int rows = SR * SETS, set_rows = SR;
+  static __device__ __forceinline__ int per_set(const ListParams& p) { return SR / p.c.G; }
+  static __device__ __forceinline__ int tiles(const ListParams& p, const Sequence& x) {
+    const int n = SETS * per_set(p);
+    return (x.count + n - 1) / n;
+  }
+  static __device__ __forceinline__ int groups(const ListParams& p, const Sequence& x, int j) {
+    const int n = SETS * per_set(p);
+    return reach_of<GT>(p, x, j * n, min(n, x.count - j * n)).groups;
+  }
 };
 struct Piece : Part {
-  int row0, rows;                                    // rows: that exist
+  int token0, tokens;                                // of the sequence's tokens
   Reach r;
 };
-template <int R, int GT>
+template <class Tiles, int GT>
 __device__ __forceinline__ Piece next_piece(Walk& walk) {
   Piece w;
   static_cast<Part&>(w) = walk.next();
   if (w.any) {
-    w.row0 = w.j * R;
-    w.rows = min(R, w.x.count * walk.p.c.G - w.row0);
-    w.r = reach_of<GT>(walk.p, w.x, w.row0, R);
+    const int n = Tiles::rows / Tiles::set_rows * Tiles::per_set(walk.p);
+    w.token0 = w.j * n;
+    w.tokens = min(n, w.x.count - w.token0);
+    w.r = reach_of<GT>(walk.p, w.x, w.token0, w.tokens);
   }
   return w;
 }
-// row of q / out (in units of d elements) of row r of a piece
-__device__ __forceinline__ long long token_head(const ListParams& p, const Piece& w, int r) {
-  const int row = w.row0 + r, t = row / p.c.G;
-  return (static_cast<long long>(w.x.cu) + t) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + (row - t * p.c.G);
+// Row rr of a set: its token in the tile (-1: there is none), and its row of q / out in units of d elements.
+template <int SR>
+__device__ __forceinline__ int row_token(const ListParams& p, int tokens, int set, int rr) {
+  const int per = SR / p.c.G, t = rr / p.c.G;
+  return t < per && set * per + t < tokens ? set * per + t : -1;
+}
+__device__ __forceinline__ long long token_head(const ListParams& p, const Sequence& x, int token, int kh, int rr) {
+  return (static_cast<long long>(x.cu) + token) * (p.c.Hkv * p.c.G) + kh * p.c.G + rr % p.c.G;
 }
 template <int R, int D>
 __device__ __forceinline__ float* record_of(const WindowParams& p, int b, bool first) { return p.partials + record_at(b, first) * (R * (D + 2)); }
 
 // Tiles that several CTAs share: a warp per row joins their records.  Blocks (b, .): the tile that share b begins in.
 constexpr int kMergeWarps = 8;
-template <int R, int D, typename T>
+template <class Tiles, int D, typename T>
 __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __grid_constant__ WindowParams p) {
   grid_dep_wait();
   const int b = blockIdx.x + 1, lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
   Share x;
   const int last = records_from(p, b, x);
   if (last < b) return;
-  Piece w;
-  w.x = x.t.x;
-  w.kh = x.kh;
-  w.row0 = x.t.j * R;
-  if (r >= w.x.count * p.c.G - w.row0) return;
+  constexpr int R = Tiles::rows, SR = Tiles::set_rows;
+  const int per = R / SR * Tiles::per_set(p), token = row_token<SR>(p, x.t.x.count - x.t.j * per, r / SR, r % SR);
+  if (token < 0) return;
   constexpr int C = D / 32, kBatch = 4;
   float acc[C], M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -120,7 +131,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __
     }
     M = top;
   }
-  const long long row = token_head(p, w, r);
+  const long long row = token_head(p, x.t.x, x.t.j * per + token, x.kh, r % SR);
   const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
   for (int c = 0; c < C; ++c) static_cast<T*>(p.out)[row * D + c * 32 + lane] = from_f32<T>(acc[c] * inv);
@@ -131,15 +142,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32) window_merge_kernel(const __
 #include "window_attn_tc.cuh"
 
 // ===================================================================== host side
-template <int R, int GT, int D, typename Launch, typename T>
+template <class Tiles, int D, typename Launch, typename T>
 int32_t with_plan(losa_ctx* c, WindowParams& p, cudaStream_t st, T, Launch&& main_kernel) {
   place_plan(c, p);
   p.partials = reinterpret_cast<float*>(c->ws + c->lay.scores);
-  launch_k(list_plan_kernel<RowTiles<R, GT>>, 1, kPlanThreads, 0, st, static_cast<const ListParams&>(p));
+  launch_k(list_plan_kernel<Tiles>, 1, kPlanThreads, 0, st, static_cast<const ListParams&>(p));
   int32_t rc = after_launch(c);
   if (rc == LOSA_OK) rc = main_kernel();
   if (rc != LOSA_OK) return rc;
-  launch_k(window_merge_kernel<R, D, T>, dim3(p.n_ctas, R / kMergeWarps), kMergeWarps * 32, 0, st, p);
+  launch_k(window_merge_kernel<Tiles, D, T>, dim3(p.n_ctas, Tiles::rows / kMergeWarps), kMergeWarps * 32, 0, st, p);
   return after_launch(c);
 }
 
@@ -154,7 +165,7 @@ int32_t launch_f32(losa_ctx* c, WindowParams& p, cudaStream_t st) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, win_smem<D>()));
     c->window_attr_set |= bit;
   }
-  return with_plan<kWinRows, kWinKeys, D>(c, p, st, float{}, [&]() -> int32_t {
+  return with_plan<WinTiles, D>(c, p, st, float{}, [&]() -> int32_t {
     launch_k(kernel, p.n_ctas, kWinThreads, win_smem<D>(), st, p);
     return after_launch(c);
   });
@@ -165,9 +176,15 @@ int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_
   using Tc = WindowTc<FMT, D, GP>;
   const int32_t rc = Tc::quant ? raw_tensor_maps(c, kv) : pool_tensor_maps(c, kv);
   if (rc != LOSA_OK) return rc;
-  CUtensorMap mk, mv;
+  CUtensorMap mk, mv, mq;
   memcpy(&mk, Tc::quant ? c->tmap_raw[0] : c->tmap_k, sizeof(mk));
   memcpy(&mv, Tc::quant ? c->tmap_raw[1] : c->tmap_v, sizeof(mv));
+  if constexpr (!Tc::quant) {
+    const int32_t rq = query_tensor_map(c, p.q.q, p.q.stride, p.q.T, 128 / p.c.G, &mq);
+    if (rq != LOSA_OK) return rq;
+  } else {
+    mq = mk;                                         // (not used)
+  }
   p.n_ctas = c->n_sms;
   p.pad = 2;
   p.least = 3;
@@ -175,14 +192,10 @@ int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_
   constexpr int bit = 1 << FMT;
   if (!(c->window_attr_set & bit)) {
     LOSA_CUDA_TRY(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc::smem));
-    // the kernel moves registers between its warps: a build that is launched with fewer than it deals out would wait for ever
-    cudaFuncAttributes fa;
-    LOSA_CUDA_TRY(c, cudaFuncGetAttributes(&fa, kernel));
-    if (fa.numRegs < Tc::launch_regs) return LOSA_ERR_UNSUPPORTED;
     c->window_attr_set |= bit;
   }
-  return with_plan<Tc::rows, kWtKeys, D>(c, p, st, __nv_bfloat16{}, [&]() -> int32_t {
-    launch_k(kernel, p.n_ctas, Tc::warps * 32, Tc::smem, st, mk, mv, p);
+  return with_plan<typename Tc::Tiles, D>(c, p, st, __nv_bfloat16{}, [&]() -> int32_t {
+    launch_k(kernel, p.n_ctas, Tc::warps * 32, Tc::smem, st, mk, mv, mq, p);
     return after_launch(c);
   });
 }

@@ -5,6 +5,7 @@
 #pragma once
 
 constexpr int kWinRows = 64, kWinKeys = 64, kWinThreads = 128;
+using WinTiles = RowTiles<kWinRows, 1, kWinKeys>;
 template <int D> constexpr int win_smem() { return (kWinRows * D + kWinKeys * (D + 4) + kWinKeys * D + kWinRows * (kWinKeys + 4)) * 4; }
 
 template <int D>
@@ -17,25 +18,23 @@ __global__ void __launch_bounds__(kWinThreads, 2) window_f32_kernel(const __grid
   grid_dep_trigger();
   grid_dep_wait();
   Walk walk(p, blockIdx.x);
-  for (Piece w = next_piece<R, GT>(walk); w.any; w = next_piece<R, GT>(walk)) {
+  for (Piece w = next_piece<WinTiles, GT>(walk); w.any; w = next_piece<WinTiles, GT>(walk)) {
     __syncthreads();
     for (int i = tid; i < R * C8; i += kWinThreads) {
       const int r = i / C8, ch = i - r * C8;
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = 0.f;
-      if (r < w.rows) {
-        const int row = w.row0 + r, t = row / p.c.G;
-        load8(static_cast<const T*>(p.q.q) + (static_cast<long long>(w.x.cu) + t) * p.q.stride + (w.kh * p.c.G + row - t * p.c.G) * D + ch * 8, v);
-      }
+      const int t = row_token<R>(p, w.tokens, 0, r);
+      if (t >= 0) load8(static_cast<const T*>(p.q.q) + (static_cast<long long>(w.x.cu) + w.token0 + t) * p.q.stride + (w.kh * p.c.G + r % p.c.G) * D + ch * 8, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) sq[r * D + ch * 8 + k] = v[k];
     }
     int2 sees[8];                                    // keys of this thread's rows: below x, from y on or below the sinks
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int r = ty * 8 + i;
-      sees[i] = r < w.rows ? keys_of(p.q, w.x, w.x.start + (w.row0 + r) / p.c.G) : make_int2(0, 0);
+      const int t = row_token<R>(p, w.tokens, 0, ty * 8 + i);
+      sees[i] = t >= 0 ? keys_of(p.q, w.x, w.x.start + w.token0 + t) : make_int2(0, 0);
     }
     float m[8], l[8], o[8][NC * 4];
 #pragma unroll
@@ -154,9 +153,10 @@ __global__ void __launch_bounds__(kWinThreads, 2) window_f32_kernel(const __grid
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
       const int r = ty * 8 + i;
-      if (r >= w.rows) continue;
+      const int t = row_token<R>(p, w.tokens, 0, r);
+      if (t < 0) continue;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      const long long row = token_head(p, w, r);
+      const long long row = token_head(p, w.x, w.token0 + t, w.kh, r);
 #pragma unroll
       for (int h = 0; h < NC; ++h)
 #pragma unroll
