@@ -152,6 +152,21 @@ class LosaLayer:
         """The tokens' queries and keys rotated, with nothing appended (a denoising step's inputs)."""
         B.losa_rope_append(self.ctx, None, rope, tokens)
 
+    def attend(self, queries, out, lse=None):
+        """New tokens over the cache, each over the keys it sees (binding.make_queries: a window, first tokens that stay visible)."""
+        B.losa_window_attn(self.ctx, queries, self.kv, out, lse)
+
+    def add_weights(self, queries, lse, keep=1.0):
+        """What the cached tokens receive from new ones, added to keep * kv_weights (allocated by the first call)."""
+        if not hasattr(self, "kv_weights"):
+            pool = self.kv._keep[0]
+            self.kv_weights = torch.zeros(pool.shape[0], self.cfg.n_kv_heads, self.cfg.page_size, dtype=torch.float32, device=self.device)
+        B.losa_kv_weights(self.ctx, queries, self.kv, lse, self.kv_weights, keep)
+
+    def evict(self, eviction):
+        """Sequences cut down to their budgets (binding.make_eviction) by the weights that add_weights has gathered."""
+        B.losa_kv_evict(self.ctx, self.kv, self.kv_weights, eviction)
+
     def finalize_block(self, k_blk, v_blk):
         B.losa_update_prefix_cache(self.ctx, self.kv, self.state, None, k_blk, v_blk, True)
 
