@@ -71,11 +71,13 @@ __global__ void __launch_bounds__(kChooseThreads, 1) evict_choose_kernel(const _
   const int first = min(p.sinks, b), tail = L - min(p.recent, b - first);      // candidates: first .. tail - 1
   uint32_t want = b - first - (L - tail);
   const bool in_smem = L <= kChooseHeld;
+  const int g_log = __ffs(p.c.g) - 1;
   auto from_cache = [&](int j) {
-    const int page = p.c.page_table[static_cast<size_t>(s) * p.c.Pmax + j / p.c.g];
-    return weight_order(p.weights[(static_cast<size_t>(page) * p.c.Hkv + kh) * p.c.g + j % p.c.g]);
+    const int page = p.c.page_table[static_cast<size_t>(s) * p.c.Pmax + (j >> g_log)];
+    return weight_order(p.weights[((static_cast<size_t>(page) * p.c.Hkv + kh) << g_log) + (j & (p.c.g - 1))]);
   };
   if (in_smem) {
+#pragma unroll 8
     for (int j = tid; j < L; j += kChooseThreads) held[j] = from_cache(j);
     __syncthreads();
   }
@@ -258,8 +260,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
       if (lane == 0) amax[t][warp] = top[t];
     }
   }
-  __threadfence();                                   // every thread's loads are done before the page is said to be read
-  __syncthreads();
+  __syncthreads();                                   // (with it the release below is every thread's: their loads come before it)
   if (tid == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(read + c), "r"(1u) : "memory");
   if constexpr (FMT == kRowsFp8) {
 #pragma unroll
