@@ -144,8 +144,8 @@ int32_t losa_destroy(losa_ctx* ctx);
  * (LOSA_ERR_TIMEOUT or LOSA_ERR_BOUNDS) and clears it, or LOSA_OK. */
 int32_t losa_poll_status(losa_ctx* ctx, void* stream);
 
-/* Bound of the waits inside the bf16 stage-4 kernel and the kernel for more than 16 query rows per KV
- * head over 4-bit pages (their warps hand work to one another through shared-memory barriers), in SM clock cycles; `cycles` <= 0 restores the default of about one
+/* Bound of the waits inside the bf16 stage-4 kernel, the kernel for more than 16 query rows per KV
+ * head over 4-bit pages, losa_window_attn and losa_kv_weights on bf16 and quantised pages, and losa_kv_evict (its pages wait for earlier ones; their warps hand work to one another through shared-memory barriers), in SM clock cycles; `cycles` <= 0 restores the default of about one
  * second.  A wait that outlasts the bound makes its thread block record LOSA_ERR_TIMEOUT, wait
  * (again within a bound) for the page copies and tensor-core instructions it had already started,
  * release its tensor memory and return: the launch ends normally, the step's results are
@@ -463,7 +463,8 @@ typedef struct {
  * quantised again from their dequantised rows as by block finalisation, their slots behind b hold code 0 then.  kmin / kmax of these pages are recomputed (left out when both are NULL) and
  * kv_len[s] = b.  Only the first b entries of kept are written.  Places behind b keep what they held (but for FP8's last page); pages behind ceil(b / g) are the
  * caller's to hand out again.  Pages that a sequence shares with another must not be evicted from.  A sequence whose length is not in 0 .. P_max * g, whose budget is
- * above kept_stride, or one of whose pages is not of the pool, is left as it is and reported (LOSA_ERR_BOUNDS). */
+ * above kept_stride, or one of whose pages is not of the pool, is left as it is and reported (LOSA_ERR_BOUNDS).  After LOSA_ERR_TIMEOUT (a wait limit that
+ * ran out) rows of the call's sequences are moved in part: their cache is lost. */
 int32_t losa_kv_evict(losa_ctx* ctx, losa_kv_t* kv, float* weights, const losa_eviction_t* ev, void* stream);
 
 /* Set-up helper — per-page min/max keys of Section 2.3 for the whole prefix: kmin/kmax of every

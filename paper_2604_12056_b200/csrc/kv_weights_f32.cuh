@@ -1,5 +1,6 @@
 // The keys' weights in fp32 on the CUDA cores: included by kv_weights.cu (same namespace).
 //
+// fp32 products stay on the CUDA cores, as stage 4's do; shared memory bounds them (twelve 16-byte reads for 128 products).
 // A CTA has 64 keys and takes 64 rows at a time, 8 rows by 4 keys a thread.
 #pragma once
 

@@ -109,7 +109,7 @@ template <int FMT, int D, int GP, bool HALF>
 __device__ __forceinline__ void raw_convert(const uint8_t* raw, uint8_t* tile, int id) {
   using Raw = RawTile<FMT, D, GP>;
   constexpr int E = 128 / RowFormat<FMT>::bits;      // elements of a piece
-#pragma unroll 2
+#pragma unroll 1
   for (int i = id; i < 128 * Raw::pieces; i += 128) {
     const int t = i / Raw::pieces, piece = i % Raw::pieces;
     const uint4 u = *reinterpret_cast<const uint4*>(raw + i * 16);

@@ -186,8 +186,10 @@ int32_t launch_tc(losa_ctx* c, WindowParams& p, const losa_kv_t* kv, cudaStream_
     mq = mk;                                         // (not used)
   }
   p.n_ctas = c->n_sms;
-  p.pad = 2;
-  p.least = 3;
+  // Entering a tile costs a CTA as much as this many groups, or a little less where tiles are many.  2, 4, 5, 6 groups, us: blocks of 32 tokens over windows of 4,096
+  // 57.3, 56.4, 54.3, 53.5, decoded tokens over FP8 caches 123, 118, 116, 118, over windows of 512 62.8, 63.7, 62.8, 63.5; ragged prompts with a window of 1,024 with 2 and 4 473, 480.
+  p.pad = p.q.max_tokens <= 128 / p.c.G ? 5 : 2;
+  p.least = p.pad + 1;
   auto kernel = window_tc_kernel<FMT, D, GP>;
   constexpr int bit = 1 << FMT;
   if (!(c->window_attr_set & bit)) {
