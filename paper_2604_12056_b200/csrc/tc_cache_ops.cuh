@@ -19,11 +19,6 @@ __device__ __forceinline__ void tma_load_queries(uint32_t dst, const CUtensorMap
                ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(head), "r"(token) : "memory");
 }
 // two at a time
-__device__ __forceinline__ float max3_f32(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ float2 fma2_f32(float2 a, float2 b, float2 c) {
   float2 d;
   asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
