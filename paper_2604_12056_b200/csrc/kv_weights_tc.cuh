@@ -222,10 +222,9 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
       __syncwarp();
       ++n;
     }
-    // (what is in flight has landed before the CTA's shared memory is given up)
+    // (what is in flight has landed before the CTA's shared memory is given up, whichever warp's wait has run out)
     constexpr int slots = QUANT ? NR : NK;
-    if (!ok)
-      for (int i = 0; i < min(slots, n); ++i) mbar_drain((QUANT ? r_full : k_full) + 8 * i, ((n - 1 - i) / slots) & 1);
+    for (int i = 0; i < min(slots, n); ++i) mbar_drain((QUANT ? r_full : k_full) + 8 * i, ((n - 1 - i) / slots) & 1);
     __syncwarp();
   } else if (warp == kKwMmaWarp) {
     // ================================================================== K Q^T
@@ -315,8 +314,8 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
         begun = job;
       }
     }
-    // (what is in flight has landed before the CTA's shared memory is given up)
-    if (!ok && begun >= 0) mbar_drain(q_full + 8 * (begun % NQ), (begun / NQ) & 1);
+    // (likewise)
+    if (begun >= 0) mbar_drain(q_full + 8 * (begun % NQ), (begun / NQ) & 1);
     __syncwarp();
   }
   tc5_fence_before();

@@ -461,8 +461,9 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
           if (v == 0 && gi == first) {
 #pragma unroll 1
             for (int t = 0; t < (w.joint ? 1 : 2); ++t) {
-              const int before = t ? nq1++ : nq0++;
+              const int before = t ? nq1 : nq0;
               if (before > 0 && !wait(q_free + 8 * t, (before - 1) & 1)) { ++g; return false; }
+              t ? ++nq1 : ++nq0;
               if (elect_one()) {
                 mbar_expect_tx(q_full + 8 * t, per * p.c.G * D * 2);
 #pragma unroll
@@ -475,15 +476,14 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       }
       return ok;
     };
-    // what is in flight has landed before the CTA's shared memory is given up
+    // What is in flight has landed before the CTA's shared memory is given up.  Whoever gave up: another warp's wait may have run out when this one has begun its last
+    // copies and has nothing left to wait for.
     auto settle = [&]() {
       const int v = warp == kWtValueWarp, slots = QUANT ? NR : v ? NV : NK;
       const uint32_t full = QUANT ? r_full + 8 * NR * v : v ? v_full : k_full;
-      if (!ok) {
-        for (int i = 0; i < min(slots, g); ++i) mbar_drain(full + 8 * i, ((g - 1 - i) / slots) & 1);
-        if (!QUANT && nq0 > 0) mbar_drain(q_full, (nq0 - 1) & 1);
-        if (!QUANT && nq1 > 0) mbar_drain(q_full + 8, (nq1 - 1) & 1);
-      }
+      for (int i = 0; i < min(slots, g); ++i) mbar_drain(full + 8 * i, ((g - 1 - i) / slots) & 1);
+      if (!QUANT && nq0 > 0) mbar_drain(q_full, (nq0 - 1) & 1);
+      if (!QUANT && nq1 > 0) mbar_drain(q_full + 8, (nq1 - 1) & 1);
       __syncwarp();
     };
     if (warp == kWtLoadWarp) {

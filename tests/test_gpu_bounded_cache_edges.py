@@ -1,0 +1,42 @@
+"""What a bounded cache's calls do at their edges: waits that run out with work begun, padding tokens, sequences that are left out, what is
+no number on quantised pages (needs a B200)."""
+import pytest
+import torch
+
+import bounded_cache_ref as ref
+from bounded_cache_ref import Cache
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = ["f32", "bf16", "fp8", "int4"]
+QUICK = [40, 100, 300, 700, 1000, 1500, 2200, 3000, 4500, 6000, 9000, 12000, 25000]      # cycles: from a look at a barrier to more than most waits take
+
+
+def weights_of(c, w, mask=(0, 0, 1), keep=1.0):
+    """The weights after a call on a copy of w, and the status."""
+    w = w.clone()
+    c.B.losa_kv_weights(c.ctx, c.queries(*mask), c.kv, c.lse, w, keep)
+    return w, c.ctx.poll_status()
+
+
+# prompts, blocks, single tokens: pieces that one set of warps or both work on, many short ones and few long ones
+BATCHES = [([700, 300, 64], [100, 1, 64]), ([4000] * 3, [1, 1, 1]), ([90] * 40, [1] * 40), ([600] * 20, [32] * 20), ([2500], [2500])]
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "int4"])
+@pytest.mark.parametrize("lens,new", BATCHES)
+def test_weights_whose_waits_run_out_with_work_begun(fmt, lens, new):
+    """Bounds at which some warps may give up while others have copies and products in flight: the call ends, right or reported, and the next one is right."""
+    c = Cache(lens, fmt=fmt)
+    c.tokens(new, [L - n for L, n in zip(lens, new)])
+    assert c.attend(0, 0, 1) == 0
+    zero = torch.zeros(c.kp.shape[0], c.hkv, c.g, device="cuda")
+    right, status = weights_of(c, zero)
+    assert status == 0
+    for limit in QUICK:
+        c.ctx.set_wait_limit(limit)
+        got, status = weights_of(c, zero)
+        assert status == c.B.LOSA_ERR_TIMEOUT or (status == 0 and torch.equal(got, right)), limit
+        c.ctx.set_wait_limit(0)
+        got, status = weights_of(c, zero)
+        assert status == 0 and torch.equal(got, right), limit
