@@ -36,7 +36,7 @@ template <int FMT, int D, int GP> struct WindowTc {
   // shared memory: tiles, barriers, [quantised pages: the rows' scales,] notes, exchange between the sets
   static constexpr int bars = rows / 128 * qtile + (nk + nv) * tile + 2 * nr * raw;
   static constexpr int scales = bars + 512, notes = scales + (quant ? 512 : 0), sets = quant ? 0 : notes + kWtAhead * kWtNote * 4;
-  static constexpr int smem = notes + kWtAhead * kWtNote * 4 + (quant ? 0 : 1024);       // (quantised pages: the sets meet in the tile of Q, once the products have run)
+  static constexpr int smem = notes + kWtAhead * kWtNote * 4 + (quant ? 0 : 2048);       // (quantised pages: the sets meet in the tile of Q, once the products have run)
   static_assert(smem <= 232448, "shared memory");
 };
 
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
   constexpr int kOdd = 8;
   static_assert(kOdd > NV + 1, "pieces ahead");
   volatile int* odd_piece = reinterpret_cast<volatile int*>(gen + Tc::bars + 408);
-  float2* exchange = reinterpret_cast<float2*>(gen + Tc::sets);          // [128] reference and sum of one set's rows, at the end of a piece that both sets have
+  float2* exchange = reinterpret_cast<float2*>(gen + Tc::sets);          // [set][128] reference and sum of the sets' rows, at the end of a piece that both sets have
   [[maybe_unused]] float* xs = reinterpret_cast<float*>(gen + Tc::scales);       // [128] quantised pages: what a row's scores are multiplied by
   const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
 
@@ -159,9 +159,18 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
     const int set = warp >> 2, at128 = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_at = tmem + COL_S + set * 128 + lanes, o_at = tmem + COL_O + set * 128 + lanes;
+    // The sets meet in pieces that both of them have, and a meeting has no bound.  So all eight warps agree before such a piece, and before they leave the list: one
+    // that has given up does not hear of the piece that the others go on to, and takes them with it here.  Within the piece nobody leaves.
     auto all_meet = [&]() {
       __syncwarp();
       asm volatile("bar.sync 1, %0;" ::"n"(kWtSoftWarps * 32) : "memory");
+    };
+    auto all_go_on = [&](bool mine) {
+      uint32_t all;
+      __syncwarp();
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 2, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                   : "=r"(all) : "r"(static_cast<int>(mine)), "n"(kWtSoftWarps * 32) : "memory");
+      return all != 0;
     };
     // fp16 weights are taken times 2^7, so that they keep eleven bits down to 2^-21 of a row's largest and are within 2^-32 of it below
     constexpr float kLift = QUANT ? 7.f : 0.f;
@@ -197,7 +206,8 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
     Note w = next();
     write_q(w);
     int n = 0, pieces = 0, ends = 0;                 // jobs of this set before; pieces so far, and those in which the set had a job
-    while (w.any) {
+    while (true) {
+      if ((!w.any || w.joint) && !all_go_on(w.any)) break;
       float sc = p.scale_log2;
       const bool both = w.joint;
       const int turn = set ^ w.flip;                 // which half of the tile, or which of every two groups, is this set's
@@ -315,16 +325,11 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       bool use0 = had && m != kWtNone, use1 = false;
       if (both) {
         if constexpr (QUANT) all_meet();
-        float2 mine = make_float2(M, l), theirs;
-        if (set == 1) exchange[at128] = mine;
+        const float2 mine = make_float2(M, l);
+        exchange[tid] = mine;
         tc5_fence_before();
         all_meet();
-        if (set == 0) {
-          theirs = exchange[at128];
-          exchange[at128] = mine;
-        }
-        all_meet();
-        if (set == 1) theirs = exchange[at128];
+        const float2 theirs = exchange[tid ^ 128];
         tc5_fence_after();
         const float2 e0 = set ? theirs : mine, e1 = set ? mine : theirs;
         top = fmaxf(e0.x, e1.x);

@@ -40,3 +40,23 @@ def test_weights_whose_waits_run_out_with_work_begun(fmt, lens, new):
         c.ctx.set_wait_limit(0)
         got, status = weights_of(c, zero)
         assert status == 0 and torch.equal(got, right), limit
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "int4"])
+@pytest.mark.parametrize("lens,new", BATCHES)
+def test_attention_whose_waits_run_out_with_work_begun(fmt, lens, new):
+    """Likewise for the attention, whose two sets of warps meet at the end of a piece."""
+    c = Cache(lens, fmt=fmt)
+    c.tokens(new, [L - n for L, n in zip(lens, new)])
+    for limit in QUICK:
+        c.ctx.set_wait_limit(limit)
+        status = c.attend(0, 0, 1)
+        assert status in (0, c.B.LOSA_ERR_TIMEOUT), limit
+        if status == 0:
+            c.check()
+        c.ctx.set_wait_limit(0)
+        c.out.fill_(55)
+        assert c.attend(0, 0, 1) == 0
+        right = c.out.clone() if limit == QUICK[0] else right
+        assert torch.equal(c.out, right), limit
+    c.check()
