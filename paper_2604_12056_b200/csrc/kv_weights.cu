@@ -106,7 +106,7 @@ int32_t launch_kv_weights(losa_ctx* c, const losa_queries_t* q, const losa_kv_t*
   p.weights = weights;
   p.keep = keep;
   p.status = status_ptr(c);
-  p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
+  set_bounds(c, p);
   p.scale_log2 = c->shape.sm_scale * kLog2e;
   auto run = [&](auto f, auto d) -> int32_t {
     constexpr int FMT = decltype(f)::value, D = decltype(d)::value;

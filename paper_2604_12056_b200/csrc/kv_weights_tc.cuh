@@ -109,9 +109,7 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
   __syncthreads();
   tc5_fence_after();
   const uint32_t tmem = warp_uniform(*tmem_slot);
-  // a bound shorter than a look at a barrier takes has run out by then (which is how the way out is exercised)
-  bool ok = p.wait_cycles >= kLookCycles;
-  if (!ok && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
+  bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (ok) ok = warp_mbar_wait(bar, parity, abort_flag, p.status, p.wait_cycles);
     __syncwarp();                                    // (what follows is for whole warps)
@@ -199,6 +197,11 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
     int n = 0;
     for (KeyPiece w = next_keys(walk); w.any && ok; w = next_keys(walk)) {
       if (w.last == w.first) continue;
+      if (n >= p.copies) {
+        *abort_flag = 1;
+        if (lane == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
+        break;
+      }
       const int slot = n % (QUANT ? NR : NK), key = w.key0 + lane * GP;
       int page = -1;
       if (lane < PG && key < w.x.len) page = max(0, page_of(p.c, w.s, key / GP, p.status));

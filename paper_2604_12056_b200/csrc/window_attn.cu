@@ -212,7 +212,7 @@ int32_t launch_window_attn(losa_ctx* c, const losa_queries_t* q, const losa_kv_t
   p.lse = lse_opt;
   p.status = status_ptr(c);
   p.scale_log2 = c->shape.sm_scale * kLog2e;
-  p.wait_cycles = c->wait_cycles > 0 ? c->wait_cycles : kWaitCycles;
+  set_bounds(c, p);
   auto run = [&](auto f, auto d) -> int32_t {
     constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
     if constexpr (FMT == kRowsF32) {

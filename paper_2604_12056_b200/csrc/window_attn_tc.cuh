@@ -119,9 +119,7 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
   __syncthreads();
   tc5_fence_after();
   const uint32_t tmem = warp_uniform(*tmem_slot);
-  // a bound shorter than a look at a barrier takes has run out by then (which is how the way out is exercised)
-  bool ok = p.wait_cycles >= kLookCycles;
-  if (!ok && tid == 0) set_status(p.status, LOSA_ERR_TIMEOUT);
+  bool ok = true;
   // (written out small: there are dozens of waits, and the loops have to stay in the instruction cache)
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (ok) {
@@ -442,6 +440,11 @@ __global__ void __launch_bounds__(WindowTc<FMT, D, GP>::warps * 32, 1) window_tc
       int pages = 0;                                 // of the next 32 / PG groups, one per lane; -1: nobody sees it
       [[maybe_unused]] float scale = 0.f;            // FP8: theirs
       for (int gi = first; gi < last; ++gi, ++g) {
+        if (g >= p.copies) {
+          *abort_flag = 1;
+          ok = false;
+          return false;
+        }
         const int i = (gi - first) % (32 / PG), slot = g % slots, turns = g / slots;
         if (i == 0) {
           const int mine = gi + lane / PG, key = mine < last ? w.key(mine) + (lane % PG) * GP : w.end;

@@ -25,6 +25,7 @@ struct ListParams {
   float keep;                                        // weights only
   int32_t* status;
   long long wait_cycles;
+  int copies;                                        // groups of keys or values after which the warps that copy them give up
 };
 
 // Ops: static int tiles(p, sequence); static int groups(p, sequence, j).
@@ -193,6 +194,15 @@ __device__ __forceinline__ int records_from(const ListParams& p, int b, Share& x
 }
 // Where a record lies, in records: the first part of a tile in its CTA's second place, the others (their CTA's first part) in the first.
 __device__ __forceinline__ size_t record_at(int b, bool first) { return static_cast<size_t>(b) * 2 + (first ? 1 : 0); }
+
+// The bound of the waits.  One of n cycles that is shorter than a look at a barrier takes holds for none; the warps that copy pages give up before their n-th group
+// instead, and the others with them: the way out is taken with copies and products in flight, whatever the hardware's speed (a look may put its warp to sleep for
+// longer than a short bound).
+inline void set_bounds(const losa_ctx* c, ListParams& p) {
+  const bool few = c->wait_cycles > 0 && c->wait_cycles < kLookCycles;
+  p.wait_cycles = c->wait_cycles > 0 && !few ? c->wait_cycles : kWaitCycles;
+  p.copies = few ? static_cast<int>(c->wait_cycles) - 1 : 0x7fffffff;
+}
 
 inline void place_plan(const losa_ctx* c, ListParams& p) {
   char* at = c->ws + c->lay.plan;

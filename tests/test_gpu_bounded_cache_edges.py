@@ -9,7 +9,7 @@ from bounded_cache_ref import Cache
 pytestmark = pytest.mark.gpu
 
 FORMATS = ["f32", "bf16", "fp8", "int4"]
-QUICK = [40, 100, 300, 700, 1000, 1500, 2200, 3000, 4500, 6000, 9000, 12000, 25000]      # cycles: from a look at a barrier to more than most waits take
+QUICK = [*range(1, 32), 40, 100, 300, 1000, 3000, 10000, 25000]         # cycles: below 32 the group of keys before which copies end, then bounds that some waits may not keep
 
 
 def weights_of(c, w, mask=(0, 0, 1), keep=1.0):
@@ -60,3 +60,18 @@ def test_attention_whose_waits_run_out_with_work_begun(fmt, lens, new):
         right = c.out.clone() if limit == QUICK[0] else right
         assert torch.equal(c.out, right), limit
     c.check()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "int4"])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 8])
+def test_copies_end_before_the_nth_group(fmt, n):
+    """Long sequences, so that blocks have more groups and tiles than that: always reported."""
+    c = Cache([30000, 30000], fmt=fmt, hkv=4, G=1)
+    c.tokens([700, 700], [29300, 29300])
+    assert c.attend(0, 0, 1) == 0
+    out = c.out.clone()
+    c.ctx.set_wait_limit(n)
+    assert weights_of(c, torch.zeros(c.kp.shape[0], c.hkv, c.g, device="cuda"))[1] == c.B.LOSA_ERR_TIMEOUT
+    assert c.attend(0, 0, 1) == c.B.LOSA_ERR_TIMEOUT
+    c.ctx.set_wait_limit(0)
+    assert c.attend(0, 0, 1) == 0 and torch.equal(c.out, out)
