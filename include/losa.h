@@ -151,7 +151,8 @@ int32_t losa_poll_status(losa_ctx* ctx, void* stream);
  * release its tensor memory and return: the launch ends normally, the step's results are
  * meaningless, and the context stays usable.  A bound of a few cycles makes every launch end this
  * way, which is how the path is exercised without starving any barrier: under one of n < 32 cycles the warps of losa_window_attn and losa_kv_weights that
- * copy pages give up before their n-th group of 128 tokens, with the work begun that came before (a launch whose blocks all have fewer ends as usual).  Host-side switch; takes
+ * copy pages give up before their n-th group of 128 tokens, with the work begun that came before (a launch whose blocks all have fewer ends as usual); under any of them
+ * losa_kv_evict moves the first page of each head alone.  Host-side switch; takes
  * effect for calls issued after it returns (a captured graph keeps the bound it was captured with). */
 int32_t losa_set_wait_limit(losa_ctx* ctx, int64_t cycles);
 

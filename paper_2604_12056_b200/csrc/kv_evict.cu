@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
       for (int e = 0; e < E; ++e) { lows[warp][col * E + e] = lo[e]; highs[warp][col * E + e] = hi[e]; }
   }
   // the earlier pages of this head have been read
-  bool ok = true;
+  bool ok = c == 0 || p.wait_cycles >= kLookCycles;  // (a bound shorter than a look has run out)
   for (int i = tid; i < c && ok; i += kMoveThreads) {
     if (load_acquire(read + i)) continue;
     const long long t0 = clock64();

@@ -75,3 +75,23 @@ def test_copies_end_before_the_nth_group(fmt, n):
     assert c.attend(0, 0, 1) == c.B.LOSA_ERR_TIMEOUT
     c.ctx.set_wait_limit(0)
     assert c.attend(0, 0, 1) == 0 and torch.equal(c.out, out)
+
+
+@pytest.mark.parametrize("limit", [1, 31])
+def test_eviction_under_a_bound_below_a_look_moves_first_pages_alone(limit):
+    """Pages with others before them give up: always reported, whatever stood ready, and rows behind the first page are as before; a head of one page waits for nothing."""
+    for lens, moved in (([2011, 700], 32), ([60, 33], 30)):
+        c = Cache(lens, fmt="bf16", d=64)
+        w = torch.rand(c.kp.shape[0], c.hkv, c.g, generator=c.gen, device="cuda")
+        length, budget = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, [L // 2 for L in lens]))
+        kept = torch.zeros(len(lens), c.hkv, max(lens) // 2, dtype=torch.int32, device="cuda")
+        before = c.rows("k")
+        c.ctx.set_wait_limit(limit)
+        c.B.losa_kv_evict(c.ctx, c.kv, w, c.B.make_eviction(length, budget, kept))
+        assert c.ctx.poll_status() == (c.B.LOSA_ERR_TIMEOUT if moved == 32 else 0)
+        for s, rows in enumerate(c.rows("k")):
+            for h in range(c.hkv):
+                n = min(moved, lens[s] // 2)
+                assert torch.equal(rows[:n, h], before[s][kept[s, h, :n].cpu().long(), h]) and torch.equal(rows[32:, h], before[s][32:, h])
+        c.ctx.set_wait_limit(0)
+        assert c.ctx.poll_status() == 0
