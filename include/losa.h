@@ -426,7 +426,7 @@ typedef struct {
   const int32_t* cu;        /* [N+1] first token of each sequence; cu[N] <= T; sequences may have none */
   const int32_t* start;     /* [N] place of each sequence's first token                             */
   int32_t n_tokens;         /* T, at most N * (P_max * g + B), and 2^26                              */
-  int32_t max_tokens;       /* the most tokens any sequence has (1: a decoding step)                */
+  int32_t max_tokens;       /* the most tokens any sequence has (1: a decoding step), >= 0           */
   int32_t window;           /* keys before (and with) its own place that a token sees; 0: all       */
   int32_t sinks;            /* first keys that stay visible                                         */
   int32_t span;             /* >= 1, at most LOSA_MAX_SPAN                                          */

@@ -101,7 +101,7 @@ int32_t check_kv(const losa_ctx* c, const losa_kv_t* kv, bool need_summaries) {
 
 // The tokens of a call over the cache.
 int32_t check_queries(const losa_ctx* c, const losa_queries_t* q) {
-  if (!q || !q->cu || !q->start || q->n_tokens < 0 || q->window < 0 || q->sinks < 0 || q->span < 1 || q->span > LOSA_MAX_SPAN) return LOSA_ERR_INVALID_ARG;
+  if (!q || !q->cu || !q->start || q->n_tokens < 0 || q->max_tokens < 0 || q->window < 0 || q->sinks < 0 || q->span < 1 || q->span > LOSA_MAX_SPAN) return LOSA_ERR_INVALID_ARG;
   const losa_shape_t& sh = c->shape;
   if (q->n_tokens > (1 << 26) || q->n_tokens > sh.batch * max_new_tokens(&sh)) return LOSA_ERR_UNSUPPORTED;
   if (q->n_tokens == 0) return LOSA_OK;              // (no rows: their pointer may be null)
