@@ -20,7 +20,7 @@ template <int FMT, int D, int GP> struct WeightsTc {
   static constexpr int warps = quant ? 16 : 13;
   static constexpr int nk = quant ? 2 : 3, nq = q_warps, nr = 3; // tiles of keys, of rows (one per warp that fills them: it waits for every one of its phases in turn); of keys as they lie
   static constexpr int tile = 128 * D * 2, raw = quant ? RawTile<FMT, D, GP>::bytes : 0;
-  static constexpr int norms = (nk + nq) * tile + (quant ? nr * raw : 0), other = norms + nq * kKwRows * 4, tail = other + 2 * kKwKeys * 4;
+  static constexpr int norms = (nk + nq) * tile + (quant ? nr * raw : 0), other = norms + nq * kKwRows * 4, gives = other + 2 * kKwKeys * 4, tail = gives + nq * kKwRows / 8;
   static constexpr int smem = 1024 + tail + 256;
   static_assert(smem <= 232448, "shared memory");
 };
@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
   const uint32_t kring = base, qring = kring + NK * TILE;
   [[maybe_unused]] constexpr int RAW = (NK + NQ) * TILE;                 // quantised pages as they lie
   float* norms = reinterpret_cast<float*>(gen + Tc::norms);              // [slot][row] log-normaliser in log2 units
+  uint32_t* gives = reinterpret_cast<uint32_t*>(gen + Tc::gives);        // [slot][row / 32] rows that give anything
   float* other = reinterpret_cast<float*>(gen + Tc::other);              // [2][key] the second set's sums, by turns
   const uint32_t bars = base + Tc::tail;
   const uint32_t k_full = bars, k_free = k_full + 8 * NK, q_full = k_free + 8 * NK, q_free = q_full + 8 * NQ;
@@ -139,13 +140,15 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
         if (!wait(s_full + 8 * buf, (job / kKwBufs) & 1)) break;
         tc5_fence_after();
         const float* norm = norms + slot * kKwRows;
+        const uint32_t* give = gives + slot * (kKwRows / 32);
 #pragma unroll 1
         for (int c = 0; c < n; c += 32) {
           uint32_t x[32];
           tc5_ld32_nowait(tmem + buf * 128 + c + lanes, x);
           tc5_wait_ld();
           tc5_pin32(x);
-          const uint32_t on = part ? low_bits(b - c) & ~low_bits(a - c) : 0xffffffffu;
+          const uint32_t rows = give[c >> 5], on = part ? low_bits(b - c) & ~low_bits(a - c) & rows : rows;
+          const bool mask = part || rows != 0xffffffffu;       // (a row that gives nothing may have any scores)
 #pragma unroll
           for (int k = 0; k < 32; k += 4) {
             const float4 l = *reinterpret_cast<const float4*>(norm + c + k);
@@ -155,7 +158,7 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
             e.y = ex2(e.y);
             f.x = ex2(f.x);
             f.y = ex2(f.y);
-            if (part) {
+            if (mask) {
               e.x = (on >> k) & 1u ? e.x : 0.f;
               e.y = (on >> (k + 1)) & 1u ? e.y : 0.f;
               f.x = (on >> (k + 2)) & 1u ? f.x : 0.f;
@@ -306,7 +309,11 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
         for (int i = 0; i < 4; ++i) l[i] = tok[i] < n ? p.lse[(t0 + tok[i]) * (p.c.Hkv * p.c.G) + w.kh * p.c.G + head[i]] : -INFINITY;
         if (job >= NQ && !wait(q_free + 8 * slot, (job / NQ - 1) & 1)) break;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) norms[slot * kKwRows + lane + 32 * i] = l[i] == -INFINITY ? INFINITY : l[i] * kLog2e;
+        for (int i = 0; i < 4; ++i) {
+          norms[slot * kKwRows + lane + 32 * i] = l[i] * kLog2e;
+          const uint32_t rows = __ballot_sync(0xffffffffu, l[i] != -INFINITY);
+          if (lane == 0) gives[slot * (kKwRows / 32) + i] = rows;
+        }
         __syncwarp();
         if (elect_one()) {
           mbar_expect_tx(q_full + 8 * slot, per * p.c.G * D * 2);

@@ -95,3 +95,23 @@ def test_eviction_under_a_bound_below_a_look_moves_first_pages_alone(limit):
                 assert torch.equal(rows[:n, h], before[s][kept[s, h, :n].cpu().long(), h]) and torch.equal(rows[32:, h], before[s][32:, h])
         c.ctx.set_wait_limit(0)
         assert c.ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_padding_tokens_give_nothing_whatever_they_hold(fmt, value):
+    """Tokens whose log-normaliser is -inf, in whole jobs, in parts of them and alone: the same bits as with ordinary queries in their rows."""
+    new = [70, 1, 33, 4]
+    c = Cache([500, 40, 33, 200], fmt=fmt)
+    c.tokens(new, [430, 39, 0, 196])
+    assert c.attend(200, 4, 1) == 0
+    dead = torch.tensor([*range(3, 60), 70, 75, 90, 104])               # (one of several in a job, a sequence's only one)
+    c.lse[dead] = -float("inf")
+    c.lse[104:, 1] = -float("inf")                                       # one head of the last sequence's tokens
+    w = torch.rand(c.kp.shape[0], c.hkv, c.g, generator=c.gen, device="cuda")
+    want, status = weights_of(c, w, (200, 4, 1))
+    assert status == 0
+    c.q[dead, :, 5:9] = value
+    c.q[104:, 1, 60] = value
+    got, status = weights_of(c, w, (200, 4, 1))
+    assert status == 0 and got.isfinite().all() and torch.equal(got, want)
