@@ -446,7 +446,8 @@ int32_t losa_window_attn(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t
  *   for j < kv_len[s] (what stands there for tokens that are new is not read).  lse [T, H_q] fp32: the tokens' log-normalisers, of losa_window_attn
  *   with the same losa_queries_t, or of a softmax over more keys (losa_block_attn_merge).  A token whose lse is -inf gives nothing.
  *   weights [n_phys_pages, H_kv, g] fp32, a weight beside every slot of the pool;  keep >= 0 and finite: 1 adds, less forgets.
- *   Sums are fp32 in an order that is fixed for a call's arguments.  Reports and limits as for losa_window_attn. */
+ *   Sums are fp32 in an order that is fixed for a call's arguments.  Reports and limits as for losa_window_attn; the weights of a sequence that is left out
+ *   stay as they are. */
 int32_t losa_kv_weights(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, void* stream);
 
 /* How far sequences are cut down. */

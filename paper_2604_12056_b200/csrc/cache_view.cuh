@@ -26,7 +26,7 @@ struct QueryParams {
   const int32_t *cu, *start;
   int T, max_tokens, window, sinks, span;
 };
-// A sequence as it is worked on: its tokens are cu .. cu + count - 1 at places start .., over len keys.
+// A sequence as it is worked on: its tokens are cu .. cu + count - 1 at places start .., over len keys.  One that is left out has start -1 and no tokens.
 struct alignas(16) Sequence { int cu, count, start, len; };
 
 // What of a sequence can be used (called by one lane per sequence where a report shall come once).
@@ -42,12 +42,12 @@ __device__ __forceinline__ Sequence sequence_of(const CacheParams& c, const Quer
   if (x.len < 0 || x.len > held) { x.len = x.len < 0 ? 0 : static_cast<int>(held); bad = true; }
   if (x.cu < 0 || next > q.T || x.count < 0 || x.start < 0 || x.start > (1 << 30)) {
     x.count = 0;
+    x.start = -1;
     bad = true;
   } else if (x.count > q.max_tokens) {
     x.count = q.max_tokens;
     bad = true;
   }
-  if (x.start < 0) x.start = 0;
   if (bad && status) set_status(status, LOSA_ERR_BOUNDS);
   return x;
 }

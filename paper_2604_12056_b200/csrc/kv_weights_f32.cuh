@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(kWgtThreads, 3) weights_f32_kernel(const __gri
   grid_dep_wait();
   const int s = blockIdx.z, kh = blockIdx.y, key0 = blockIdx.x * GT;
   const Sequence x = sequence_of(p.c, p.q, s, blockIdx.x == 0 && kh == 0 && tid == 0 ? p.status : nullptr);
-  if (key0 >= x.len) return;
+  if (key0 >= x.len || x.start < 0) return;
   const int2 seen = tokens_over(p, x, key0, min(GT, x.len - key0)), rows = make_int2(seen.x * p.c.G, seen.y * p.c.G);
   if (rows.x >= rows.y && p.keep == 1.f && key0 + GT <= x.start) return;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};

@@ -25,11 +25,12 @@ template <int FMT, int D, int GP> struct WeightsTc {
   static_assert(smem <= 232448, "shared memory");
 };
 
-// Tiles of keys that have anything to do: those under the first tokens, and from the window of the first token on; all where weights are forgotten.
+// Tiles of keys that have anything to do (none of a sequence that is left out): those under the first tokens, and from the window of the first token on; all where weights are forgotten.
 struct KeyReach { int first, from, tiles; };
 __device__ __forceinline__ KeyReach key_reach(const ListParams& p, const Sequence& x) {
   KeyReach r = {0, 0, 0};
   const int all = (x.len + kKwKeys - 1) / kKwKeys;
+  if (x.start < 0) return r;
   if (p.keep != 1.f) {
     r.tiles = all;
     return r;

@@ -115,3 +115,35 @@ def test_padding_tokens_give_nothing_whatever_they_hold(fmt, value):
     c.q[104:, 1, 60] = value
     got, status = weights_of(c, w, (200, 4, 1))
     assert status == 0 and got.isfinite().all() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("keep", [1.0, 0.5, 0.0])
+@pytest.mark.parametrize("wrong", ["start", "far", "tokens", "order"])
+def test_weights_of_a_sequence_that_is_left_out_stay(fmt, keep, wrong):
+    """A negative start, one above 2^30, tokens behind the last, tokens in descending order: reported, and the sequence's weights are as before."""
+    lens = [300, 77, 260]
+    c = Cache(lens, fmt=fmt)
+    c.tokens([5, 2, 3], [295, 75, 257])
+    assert c.attend(0, 0, 1) == 0
+    w = torch.rand(c.kp.shape[0], c.hkv, c.g, generator=c.gen, device="cuda")
+    right, status = weights_of(c, w, keep=keep)
+    assert status == 0
+    out = {"start": [1], "far": [1], "tokens": [2], "order": [1]}[wrong]
+    if wrong == "start":
+        c.start_t[1] = -5
+    elif wrong == "far":
+        c.start_t[1] = (1 << 30) + 1
+    elif wrong == "tokens":
+        c.cu[3] = 11                                  # one more than there are
+    else:
+        c.cu[1], c.cu[2] = 5, 4                       # the second has -1; the third's tokens begin one early
+        c.start_t[2] = 256
+        out = [1, 2]                                  # (the third is computed with other tokens: not looked at)
+    got, status = weights_of(c, w, keep=keep)
+    assert status == c.B.LOSA_ERR_BOUNDS
+    skip = 2 if wrong == "order" else None
+    for s in range(3):
+        if s != skip:
+            pages = c.table[s].long()
+            assert torch.equal(got[pages], (w if s in out else right)[pages]), s
