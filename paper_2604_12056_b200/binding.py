@@ -391,7 +391,8 @@ def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
 
 
 def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
-    """The softmax weight that cached tokens receive from new ones, added to keep * weights ([n_phys, H_kv, g] fp32)."""
+    """The softmax weight that cached tokens receive from new ones, added to keep * weights ([n_phys, H_kv, g] fp32).  No page may be
+    below the lengths of two sequences of the call."""
     q = queries._keep[0]
     assert weights.dtype == lse.dtype == torch.float32 and lse.numel() == q.shape[0] * q.shape[1]
     assert weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size
