@@ -448,8 +448,8 @@ int32_t losa_window_attn(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t
  *   weights [n_phys_pages, H_kv, g] fp32, a weight beside every slot of the pool;  keep >= 0 and finite: 1 adds, less forgets.
  *   Sums are fp32 in an order that is fixed for a call's arguments.  Reports and limits as for losa_window_attn; the weights of a sequence that is left out
  *   stay as they are.  A slot is read and written once for each sequence that holds it: pages that two sequences of a call share below their lengths (a common
- *   prefix) must not be weighed together, one sequence's part would be lost or `keep` applied twice.  Such sequences take calls of their own, in contexts whose
- *   page tables name them alone, with keep 1 in all calls but the first. */
+ *   prefix) must not be weighed together, one sequence's part would be lost or `keep` applied twice.  Such sequences take a call each, with keep 1 and the
+ *   others without tokens and with start = kv_len, which are not touched then. */
 int32_t losa_kv_weights(losa_ctx* ctx, const losa_queries_t* q, const losa_kv_t* kv, const float* lse, float keep, float* weights, void* stream);
 
 /* How far sequences are cut down. */

@@ -147,3 +147,40 @@ def test_weights_of_a_sequence_that_is_left_out_stay(fmt, keep, wrong):
         if s != skip:
             pages = c.table[s].long()
             assert torch.equal(got[pages], (w if s in out else right)[pages]), s
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sequences_that_share_pages_are_weighed_one_after_the_other(fmt):
+    """A common prefix: a call for each sequence, the others without tokens at their ends, gives the sum of both."""
+    c = Cache([200, 170], fmt=fmt)
+    c.tokens([3, 2], [197, 168])
+    shared = 160 // c.g
+    c.table[1, :shared] = c.table[0, :shared]
+    mask = (0, 0, 1)
+    assert c.attend(*mask) == 0
+    c.check()
+    w = torch.rand(c.kp.shape[0], c.hkv, c.g, generator=c.gen, device="cuda")
+    got, cu, start = w.clone(), c.cu.clone(), c.start_t.clone()
+    for s in (0, 1):
+        c.cu.copy_(cu)
+        c.cu[1 + s:] = c.cu[1 + s].clone()            # (the sequences before have none as well)
+        c.cu[:1 + s] = c.cu[s].clone()
+        c.start_t.copy_(torch.tensor([a if i == s else L for i, (a, L) in enumerate(zip(c.start, c.lens))], dtype=torch.int32))
+        before = got.clone()
+        got, status = weights_of(c, before, mask)
+        assert status == 0
+        other = c.table[1 - s, shared:].long()
+        assert torch.equal(got[other], before[other])
+    c.cu.copy_(cu)
+    k, q, lse, old = c.rows("k"), c.q.cpu().double(), c.lse.cpu().double(), w.cpu().double()
+    table = c.table.cpu().long()
+    want, tol = old.clone(), torch.zeros_like(old)
+    for s, tokens, ok in c.each():
+        place = torch.arange(c.lens[s])
+        page, slot = table[s, place // c.g], place % c.g
+        for h in range(c.hkv):
+            heads = slice(h * c.G, (h + 1) * c.G)
+            add, off = ref.weights(q[tokens, heads], k[s][:, h], ok, lse[tokens, heads], c.d ** -0.5, c.fmt != "f32")
+            want[page, h, slot] = torch.where(place < c.start[s], want[page, h, slot], 0.0) + add
+            tol[page, h, slot] += off + 2.0 ** -23 * want[page, h, slot]
+    assert ((got.cpu().double() - want).abs() <= tol).all()
