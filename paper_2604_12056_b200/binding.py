@@ -401,7 +401,7 @@ def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
 
 def losa_kv_evict(ctx, kv, weights, eviction):
     """Sequences cut down to their budgets: per KV head the tokens of least weight leave, the others move to the front."""
-    assert weights.dtype == torch.float32 and weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size
+    assert weights is None or (weights.dtype == torch.float32 and weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size)
     ctx._check("losa_kv_evict", _typed_lib().losa_kv_evict(ctx._h, C.byref(kv), _ptr(weights), C.byref(eviction), _stream()))
 
 

@@ -164,8 +164,8 @@ class LosaLayer:
         B.losa_kv_weights(self.ctx, queries, self.kv, lse, self.kv_weights, keep)
 
     def evict(self, eviction):
-        """Sequences cut down to their budgets (binding.make_eviction) by the weights that add_weights has gathered."""
-        B.losa_kv_evict(self.ctx, self.kv, self.kv_weights, eviction)
+        """Sequences cut down to their budgets (binding.make_eviction) by the weights that add_weights has gathered (LOSA_ERR_INVALID_ARG before it was called)."""
+        B.losa_kv_evict(self.ctx, self.kv, getattr(self, "kv_weights", None), eviction)
 
     def finalize_block(self, k_blk, v_blk):
         B.losa_update_prefix_cache(self.ctx, self.kv, self.state, None, k_blk, v_blk, True)

@@ -39,3 +39,19 @@ def test_fewer_than_no_tokens_are_refused_also_where_there_are_none(lib, dtype, 
     h.queries.n_tokens, h.queries.q = 1, h.q
     assert lib.losa_window_attn(h.handle, C.byref(h.queries), C.byref(h.kv), h.out, None, None) == B.LOSA_ERR_INVALID_ARG
     assert lib.losa_kv_weights(h.handle, C.byref(h.queries), C.byref(h.kv), h.lse, 1.0, h.weights, None) == B.LOSA_ERR_INVALID_ARG
+
+
+def test_a_layer_without_weights_is_refused(lib, monkeypatch):
+    """LosaLayer.evict before any add_weights: the library's refusal, not a missing attribute."""
+    from paper_2604_12056_b200.layer import LosaLayer
+    h = Host()
+
+    class Ctx:
+        _h, shape, _check = C.c_void_p(h.handle), B.ShapeT.from_address(h.handle), B.Context._check
+
+    layer = LosaLayer.__new__(LosaLayer)
+    layer.ctx, layer.kv = Ctx(), h.kv
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    with pytest.raises(B.LosaError) as e:
+        layer.evict(B.EvictionT(h.q, h.out, h.lse, 5, 0, 0))
+    assert e.value.code == B.LOSA_ERR_INVALID_ARG
