@@ -369,7 +369,7 @@ int32_t launch_kv_evict(losa_ctx* c, losa_kv_t* kv, float* weights, const losa_e
   p.sinks = ev->sinks;
   p.recent = ev->recent;
   const int n_sk = sh.batch * sh.n_kv_heads;
-  p.pages = std::min(sh.max_pages_per_seq, (ev->kept_stride + sh.page_size - 1) / sh.page_size);
+  p.pages = std::min(sh.max_pages_per_seq, (ev->kept_stride - 1) / sh.page_size + 1);      // (a stride may be any positive number)
   p.goes = reinterpret_cast<int32_t*>(c->ws + c->lay.scores);
   p.read = reinterpret_cast<uint32_t*>(p.goes + n_sk);
   p.ticket = reinterpret_cast<uint32_t*>(c->ws + c->lay.evict_ticket);

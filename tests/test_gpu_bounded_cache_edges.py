@@ -184,3 +184,19 @@ def test_sequences_that_share_pages_are_weighed_one_after_the_other(fmt):
             want[page, h, slot] = torch.where(place < c.start[s], want[page, h, slot], 0.0) + add
             tol[page, h, slot] += off + 2.0 ** -23 * want[page, h, slot]
     assert ((got.cpu().double() - want).abs() <= tol).all()
+
+
+def test_kept_rows_may_lie_far_apart():
+    """kept_stride is only a distance: the largest there is, with one row."""
+    c = Cache([300], fmt="bf16", hkv=1, G=4)
+    w = torch.rand(c.kp.shape[0], 1, c.g, generator=c.gen, device="cuda")
+    want = ref.stays([float(w[c.table[0, j // c.g].long(), 0, j % c.g]) for j in range(300)], 100, 4, 16)
+    length, budget = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (300, 100))
+    kept = torch.full((1, 1, 100), -1, dtype=torch.int32, device="cuda")
+    before = c.rows("k")[0]
+    ev = c.B.make_eviction(length, budget, kept, 4, 16)
+    ev.kept_stride = 2 ** 31 - 1
+    c.B.losa_kv_evict(c.ctx, c.kv, w, ev)
+    assert c.ctx.poll_status() == 0 and kept.flatten().tolist() == want
+    c.lens = [100]
+    assert torch.equal(c.rows("k")[0], before[want])
