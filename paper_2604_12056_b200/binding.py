@@ -383,9 +383,16 @@ def losa_int4_attn(ctx, q, kv, out, lse_opt=None):
     ctx._check("losa_int4_attn", _typed_lib().losa_int4_attn(ctx._h, _ptr(q), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
 
 
+def _queries_of(ctx, queries):
+    """The rows of a losa_queries_t, which have to be the context's."""
+    q, cu, _ = queries._keep
+    assert q.shape[1:] == (ctx.shape.n_q_heads, ctx.shape.head_dim) and q.dtype == torch_dtype(ctx.shape.dtype) and cu.numel() == ctx.shape.batch + 1
+    return q
+
+
 def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
     """Attention of new tokens over the cache, each over the keys it sees (a window and first tokens that stay visible)."""
-    q = queries._keep[0]
+    q = _queries_of(ctx, queries)
     assert out.numel() == q.numel() and out.dtype == q.dtype and (lse_opt is None or (lse_opt.dtype == torch.float32 and lse_opt.numel() == q.shape[0] * q.shape[1]))
     ctx._check("losa_window_attn", _typed_lib().losa_window_attn(ctx._h, C.byref(queries), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
 
@@ -393,7 +400,7 @@ def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
 def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
     """The softmax weight that cached tokens receive from new ones, added to keep * weights ([n_phys, H_kv, g] fp32).  No page may be
     below the lengths of two sequences of the call."""
-    q = queries._keep[0]
+    q = _queries_of(ctx, queries)
     assert weights.dtype == lse.dtype == torch.float32 and lse.numel() == q.shape[0] * q.shape[1]
     assert weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size
     ctx._check("losa_kv_weights", _typed_lib().losa_kv_weights(ctx._h, C.byref(queries), C.byref(kv), _ptr(lse), keep, _ptr(weights), _stream()))
@@ -402,6 +409,7 @@ def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
 def losa_kv_evict(ctx, kv, weights, eviction):
     """Sequences cut down to their budgets: per KV head the tokens of least weight leave, the others move to the front."""
     assert weights is None or (weights.dtype == torch.float32 and weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size)
+    assert eviction._keep[2].shape[:2] == (ctx.shape.batch, ctx.shape.n_kv_heads)
     ctx._check("losa_kv_evict", _typed_lib().losa_kv_evict(ctx._h, C.byref(kv), _ptr(weights), C.byref(eviction), _stream()))
 
 

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2604_12056_b200 import binding as B
 
@@ -26,6 +27,11 @@ class Host:
         self.queries = B.QueriesT(None, 0, at[6], at[7], 0, 0, 0, 0, 1)
         self.q, self.out, self.lse, self.weights = at[8:]
 
+    def ctx(self):
+        class Ctx:
+            _h, shape, _check = C.c_void_p(self.handle), B.ShapeT.from_address(self.handle), B.Context._check
+        return Ctx()
+
 
 @pytest.mark.parametrize("dtype,kv_format", [(B.LOSA_F32, B.LOSA_KV_NATIVE), (B.LOSA_BF16, B.LOSA_KV_NATIVE), (B.LOSA_BF16, B.LOSA_KV_FP8_E4M3), (B.LOSA_BF16, B.LOSA_KV_INT4)])
 @pytest.mark.parametrize("most", [-1, -2 ** 31])
@@ -46,12 +52,42 @@ def test_a_layer_without_weights_is_refused(lib, monkeypatch):
     from paper_2604_12056_b200.layer import LosaLayer
     h = Host()
 
-    class Ctx:
-        _h, shape, _check = C.c_void_p(h.handle), B.ShapeT.from_address(h.handle), B.Context._check
-
     layer = LosaLayer.__new__(LosaLayer)
-    layer.ctx, layer.kv = Ctx(), h.kv
+    layer.ctx, layer.kv = h.ctx(), h.kv
     monkeypatch.setattr(B, "_stream", lambda: None)
+    eviction = B.EvictionT(h.q, h.out, h.lse, 5, 0, 0)
+    eviction._keep = (None, None, torch.empty(2, 2, 5))
     with pytest.raises(B.LosaError) as e:
-        layer.evict(B.EvictionT(h.q, h.out, h.lse, 5, 0, 0))
+        layer.evict(eviction)
     assert e.value.code == B.LOSA_ERR_INVALID_ARG
+
+
+def test_tensors_of_another_shape_than_the_contexts_are_refused(lib, monkeypatch):
+    """Heads, their size, type or number of sequences that are not the context's would be read and written past their ends."""
+    h = Host()
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    monkeypatch.setattr(B, "_ptr", lambda t: None if t is None else 4096)
+    weights, bf16 = torch.empty(40, 2, 32), torch.bfloat16
+
+    def calls(shape=(3, 8, 128), dtype=bf16, sequences=2, kept=(2, 2, 5)):
+        """Whether each of the three calls comes as far as the library, which refuses its null pointers."""
+        q = torch.empty(shape, dtype=dtype)
+        queries, eviction = B.QueriesT(None, 0, None, None, 3, 3, 0, 0, 1), B.EvictionT(None, None, None, 5, 0, 0)
+        queries._keep = (q, torch.empty(sequences + 1), None)
+        eviction._keep = (None, None, torch.empty(kept))
+        lse = torch.empty(shape[:2])
+        for call in (lambda: B.losa_window_attn(h.ctx(), queries, h.kv, q, lse), lambda: B.losa_kv_weights(h.ctx(), queries, h.kv, lse, weights),
+                     lambda: B.losa_kv_evict(h.ctx(), h.kv, weights, eviction)):
+            try:
+                call()
+            except B.LosaError as e:
+                assert e.code == B.LOSA_ERR_INVALID_ARG
+                yield True
+            except AssertionError:
+                yield False
+
+    assert [*calls()] == [True, True, True]
+    for wrong in (dict(shape=(3, 4, 128)), dict(shape=(3, 8, 64)), dict(dtype=torch.float32), dict(sequences=1), dict(sequences=3)):
+        assert [*calls(**wrong)] == [False, False, True], wrong
+    for kept in ((2, 1, 5), (1, 2, 5)):
+        assert [*calls(kept=kept)] == [True, True, False]
