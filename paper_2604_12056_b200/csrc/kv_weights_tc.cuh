@@ -132,7 +132,8 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
       const int2 seen = tokens_over(p, w.x, key, 1);
       const int ta = seen.x - w.token0, tb = min(seen.y - w.token0, w.tokens);
       const Held held = held_weight(p, w.x, w.s, w.kh, key);             // (asked for before the sum)
-      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      // a sum for each job and one over the jobs: a chain of all the terms would lose three bits of the weights of a long prompt
+      float total = 0.f;
       for (int gi = w.first; gi < w.last; ++gi, ++job) {
         if ((job & 1) != set) continue;
         const int buf = job % kKwBufs, slot = job % NQ, n = min(per, w.tokens - gi * per) * p.c.G;
@@ -142,6 +143,7 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
         tc5_fence_after();
         const float* norm = norms + slot * kKwRows;
         const uint32_t* give = gives + slot * (kKwRows / 32);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
         for (int c = 0; c < n; c += 32) {
           uint32_t x[32];
@@ -169,6 +171,8 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
             sum[1] = add2_f32(sum[1], f);
           }
         }
+        const float2 both = add2_f32(sum[0], sum[1]);
+        total += both.x + both.y;
         tc5_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -177,8 +181,6 @@ __global__ void __launch_bounds__(WeightsTc<FMT, D, GP>::warps * 32, 1) weights_
         }
         __syncwarp();
       }
-      const float2 both = add2_f32(sum[0], sum[1]);
-      float total = both.x + both.y;
       int writer = jobs == 1 ? (job + 1) & 1 : 0;    // (the set that had the only job; a tile without any is the first one's)
       if (jobs > 1) {
         if (set == 1) other[(turn & 1) * kKwKeys + at128] = total;
