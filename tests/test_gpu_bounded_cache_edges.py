@@ -226,3 +226,38 @@ def test_weights_of_a_prompt_keep_the_bits_of_fp32(hkv, G, n):
             want[:a + 1024] += s.exp_().sum((0, 1))
         far = float((got[pages, h, place % c.g].double() - want).norm() / want.norm())
         assert far <= 2.0 ** -22, far
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "int4"])
+@pytest.mark.parametrize("new,start", [(300, 100), (1, 270), (7, 260)])
+def test_nan_on_quantised_pages_stays_where_it_is_seen(fmt, new, start):
+    """A value, or a run of them, that is NaN: rows that do not see it are as without it, rows that do are NaN there; then a key."""
+    c = Cache([400], fmt=fmt, hkv=1, G=4)
+    c.tokens([new], [start])
+    bad, cols = 250, slice(32, 64) if fmt == "int4" else slice(3, 9)
+    page, slot = int(c.table[0, bad // c.g]), bad % c.g
+
+    def spoil(pool, scale):
+        at = scale[page, 0, slot, 1:2] if fmt == "int4" else pool[page, 0, slot, cols]
+        old = at.clone()
+        at.fill_(255 if fmt == "int4" else 0x7f)
+        return lambda: at.copy_(old)
+
+    p = torch.arange(start, start + new)
+    for window, sinks in ((60, 4), (0, 0), (25, 0)):
+        sees = (p >= bad) & ((p < bad + window) | (window == 0))
+        assert c.attend(window, sinks, 1) == 0
+        c.check()
+        clean, lse = c.out.clone(), c.lse.clone()
+        restore = spoil(c.vp, c.vs)
+        assert c.attend(window, sinks, 1) == 0
+        restore()
+        got = c.out.clone()
+        assert got[sees][..., cols].isnan().all() and torch.equal(got[~sees], clean[~sees]) and torch.equal(c.lse, lse)
+        left = torch.ones(c.d, dtype=torch.bool)
+        left[cols] = False
+        assert torch.equal(got[sees][..., left], clean[sees][..., left])
+        restore = spoil(c.kp, c.ks)
+        assert c.attend(window, sinks, 1) == 0
+        restore()
+        assert c.out[sees].isnan().all() and torch.equal(c.out[~sees], clean[~sees]) and c.lse[sees].isnan().all() and torch.equal(c.lse[~sees], lse[~sees])
