@@ -261,3 +261,42 @@ def test_nan_on_quantised_pages_stays_where_it_is_seen(fmt, new, start):
         assert c.attend(window, sinks, 1) == 0
         restore()
         assert c.out[sees].isnan().all() and torch.equal(c.out[~sees], clean[~sees]) and c.lse[sees].isnan().all() and torch.equal(c.lse[~sees], lse[~sees])
+
+
+@pytest.mark.parametrize("a,b", [("bf16", "fp8"), ("int4", "bf16"), ("f32", "bf16")])
+def test_two_contexts_on_two_streams_at_once(a, b):
+    """Prompts and single tokens, attention, weights and eviction of two caches side by side: the same bits as one after the other."""
+    caches = []
+    for fmt, lens, new in ((a, [3000, 700], [3000, 64]), (b, [5000] * 4, [1] * 4)):
+        c = Cache(lens, fmt=fmt)
+        c.tokens(new, [L - n for L, n in zip(lens, new)])
+        c.w = torch.zeros(c.kp.shape[0], c.hkv, c.g, device="cuda")
+        c.length, c.budget = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, [L // 3 for L in lens]))
+        c.kept = torch.zeros(len(lens), c.hkv, max(lens) // 3, dtype=torch.int32, device="cuda")
+        c.held = [x.clone() for x in (c.kp, c.vp, c.w, c.kv_len, *([] if c.ks is None else [c.ks, c.vs]))]
+        caches.append(c)
+
+    def calls(c):
+        for x, old in zip((c.kp, c.vp, c.w, c.kv_len, *([] if c.ks is None else [c.ks, c.vs])), c.held):
+            x.copy_(old)
+        c.B.losa_window_attn(c.ctx, c.queries(1000, 4, 1), c.kv, c.out, c.lse)
+        c.B.losa_kv_weights(c.ctx, c.queries(1000, 4, 1), c.kv, c.lse, c.w)
+        c.B.losa_kv_evict(c.ctx, c.kv, c.w, c.B.make_eviction(c.length, c.budget, c.kept, 4, 16))
+
+    def state(c):
+        assert c.ctx.poll_status() == 0
+        return [x.contiguous().view(torch.uint8).clone() for x in (c.out, c.lse, c.w, c.kp, c.vp, c.kept, c.kv_len)]
+
+    want = []
+    for c in caches:
+        calls(c)
+        want.append(state(c))
+    streams = [torch.cuda.Stream() for _ in caches]
+    for _ in range(10):
+        torch.cuda.synchronize()
+        for c, stream in zip(caches, streams):
+            with torch.cuda.stream(stream):
+                calls(c)
+        torch.cuda.synchronize()
+        for c, right in zip(caches, want):
+            assert all(torch.equal(x, y) for x, y in zip(state(c), right))
