@@ -8,7 +8,8 @@
 // In place, read once and written once: a copy through a second buffer would double the traffic and need the room.  Eight sequences of up to 16,384 tokens
 // cut to 4,096: 81 us, 22 for choosing (64 CTAs, four passes over 16K weights in shared memory each) and 57 for moving 201 MB (3.5 TB/s: a chain
 // of ticket, list, page table, rows and flags per 16 KB).  With a fence per thread instead of one release after the barrier moving took 63 us; twelve CTAs per SM spill
-// and take 89.  One sequence of 8,201 FP8 tokens cut to 2,048: 19 us, latency.
+// and take 89.  One sequence of 8,201 FP8 tokens cut to 2,048: 19 us, latency.  A page looks at the flags of all pages before it, though at most two want its rows, so that
+// looks grow with the square of the pages: 60,001 tokens of 8 heads cut to 59,000 take 335 us in pages of 16 tokens, 280 in pages of 32 or 64.
 #include <algorithm>
 #include <type_traits>
 

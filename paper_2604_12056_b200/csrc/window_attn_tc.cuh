@@ -7,14 +7,17 @@
 //   a warp            values likewise (a copy takes its warp 130 cycles to issue, and a group of pages of 32 has eight of either)
 //   S[128 x 128] = Q K^T, O[128 x D] += P V   one issuing warp, in the order PV(j), QK(j + 2): the tensor cores run them in order, so that the scores may replace
 //                     the weights that were read before without a word from anybody; both operands of Q K^T and V come from shared memory, P from tensor memory
-//   softmax set       a row's scores are read twice, for their maximum and for the weights (32 at a time: in registers as a whole they leave none to work with), masked where the
+//   softmax set       a row's scores are read twice, for their maximum and for the weights, 32 at a time (whole rows in registers, without a split of the registers between the
+//                     warps, were slower: 134 of 170 are in use as it is), masked where the
 //                     group is not seen whole; weights go back over the scores as 16-bit operands, in two halves, so that the products of one run while
 //                     the other is worked on.  The reference maximum only moves when it would grow by more than 2^8.  Short loops and the special function unit alone: unrolled
-//                     whole, with the next 32 scores on their way and a third of the exponentials as polynomials on the FMA units, a prompt of 16,384 tokens took 1,214 us instead of 1,160.
+//                     whole, with the next 32 scores on their way and a third of the exponentials as polynomials on the FMA units, a prompt of 16,384 tokens took 5 to 8 % longer.
+//                     Weights have the values' type, as both operands of a product must: beside bf16 pages each is off by up to 2^-8 of itself (the sum takes them unrounded), outputs are
+//                     off by 2.2e-3 where a last rounding alone is 1.7e-3; beside fp16 tiles of quantised pages by 2^-11, and 1.7e-3 remain.
 //   a warp            clears the rows of V that no row of the tile sees (they may hold anything), and where rows see different keys, what is
 //                     no finite number among them (a weight of zero would not keep it out); the rows that do see it get it at the tile's end
-// Measured: a prompt of 16,384 tokens, 32 heads, window 4,096: 1,240 us (777 TFLOP/s, 46 % of the rate of a large library product); ragged prompts of 15,164 tokens, window
-// 1,024: 471; eight decoded tokens over 8,192 keys each 65 us (4.1 TB/s), over FP8 caches of up to 16,383 tokens 116.  With the softmax left out a pass over the 16,384 tokens still takes three quarters: what
+// Measured: a prompt of 16,384 tokens, 32 heads, window 4,096: 1,210 to 1,250 us, by card (777 TFLOP/s, 46 % of the rate of a large library product); ragged prompts of 15,164 tokens, window
+// 1,024: 472, from FP8 or 4-bit pages 1,320; eight decoded tokens over 8,192 keys each 65 us (4.1 TB/s), over FP8 caches of up to 16,383 tokens 115.  With the softmax left out a pass over the 16,384 tokens still takes three quarters: what
 // bounds it is the chain products -> scores -> weights -> products of either set (each hand-over 100 to 300 cycles) more than any unit: the tensor pipe is busy for 40 %.
 // 256 rows a tile because a group's K and V (64 KB) then serve two jobs: with 128 the fill of shared memory alone would be 64 bytes a cycle.
 // Tensor memory is full: scores and output of either set, 128 columns each.  Everything is handed on by mbarriers with bounded waits.
