@@ -215,6 +215,7 @@ def make_queries(q, cu, start, max_tokens=None, window=0, sinks=0, span=1) -> Qu
     x = QueriesT(q.data_ptr(), q.stride(0) if T > 1 else q.shape[1] * q.shape[2], _ptr(cu), _ptr(start), T, T if max_tokens is None else max_tokens,
                  window, sinks, span)
     x._keep = (q, cu, start)
+    x._of = (q.shape[1], q.shape[2], q.dtype, start.numel())
     return x
 
 
@@ -223,6 +224,7 @@ def make_eviction(length, budget, kept, sinks=0, recent=0) -> EvictionT:
     assert length.dtype == budget.dtype == kept.dtype == torch.int32 and kept.dim() == 3 and length.shape == budget.shape == kept.shape[:1]
     e = EvictionT(_ptr(length), _ptr(budget), _ptr(kept), kept.shape[2], sinks, recent)
     e._keep = (length, budget, kept)
+    e._of = kept.shape[:2]
     return e
 
 
@@ -245,6 +247,8 @@ class Context:
                  max_pages_per_seq, dtype, sm_scale, device="cuda"):
         self.shape = ShapeT(batch, n_q_heads, n_kv_heads, head_dim, block_size, page_size,
                             max_pages_per_seq, dtype, sm_scale)
+        # what queries and evictions have to match (kept, because a field of a structure takes longer to read)
+        self._queries, self._kv_heads = (n_q_heads, head_dim, torch_dtype(dtype), batch), (batch, n_kv_heads)
         with torch.cuda.device(device):
             n = C.c_size_t(0)
             self._check("losa_workspace_bytes", lib().losa_workspace_bytes(C.byref(self.shape), C.byref(n)))
@@ -383,16 +387,10 @@ def losa_int4_attn(ctx, q, kv, out, lse_opt=None):
     ctx._check("losa_int4_attn", _typed_lib().losa_int4_attn(ctx._h, _ptr(q), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
 
 
-def _queries_of(ctx, queries):
-    """The rows of a losa_queries_t, which have to be the context's."""
-    q, cu, _ = queries._keep
-    assert q.shape[1:] == (ctx.shape.n_q_heads, ctx.shape.head_dim) and q.dtype == torch_dtype(ctx.shape.dtype) and cu.numel() == ctx.shape.batch + 1
-    return q
-
-
 def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
     """Attention of new tokens over the cache, each over the keys it sees (a window and first tokens that stay visible)."""
-    q = _queries_of(ctx, queries)
+    q = queries._keep[0]
+    assert queries._of == ctx._queries                    # (heads, their size, type and number of sequences)
     assert out.numel() == q.numel() and out.dtype == q.dtype and (lse_opt is None or (lse_opt.dtype == torch.float32 and lse_opt.numel() == q.shape[0] * q.shape[1]))
     ctx._check("losa_window_attn", _typed_lib().losa_window_attn(ctx._h, C.byref(queries), C.byref(kv), _ptr(out), _ptr(lse_opt), _stream()))
 
@@ -400,7 +398,8 @@ def losa_window_attn(ctx, queries, kv, out, lse_opt=None):
 def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
     """The softmax weight that cached tokens receive from new ones, added to keep * weights ([n_phys, H_kv, g] fp32).  No page may be
     below the lengths of two sequences of the call."""
-    q = _queries_of(ctx, queries)
+    q = queries._keep[0]
+    assert queries._of == ctx._queries
     assert weights.dtype == lse.dtype == torch.float32 and lse.numel() == q.shape[0] * q.shape[1]
     assert weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size
     ctx._check("losa_kv_weights", _typed_lib().losa_kv_weights(ctx._h, C.byref(queries), C.byref(kv), _ptr(lse), keep, _ptr(weights), _stream()))
@@ -409,7 +408,7 @@ def losa_kv_weights(ctx, queries, kv, lse, weights, keep=1.0):
 def losa_kv_evict(ctx, kv, weights, eviction):
     """Sequences cut down to their budgets: per KV head the tokens of least weight leave, the others move to the front."""
     assert weights is None or (weights.dtype == torch.float32 and weights.numel() == kv.n_phys_pages * ctx.shape.n_kv_heads * ctx.shape.page_size)
-    assert eviction._keep[2].shape[:2] == (ctx.shape.batch, ctx.shape.n_kv_heads)
+    assert eviction._of == ctx._kv_heads
     ctx._check("losa_kv_evict", _typed_lib().losa_kv_evict(ctx._h, C.byref(kv), _ptr(weights), C.byref(eviction), _stream()))
 
 

@@ -30,6 +30,7 @@ class Host:
     def ctx(self):
         class Ctx:
             _h, shape, _check = C.c_void_p(self.handle), B.ShapeT.from_address(self.handle), B.Context._check
+            _queries, _kv_heads = (8, 128, torch.bfloat16, 2), (2, 2)
         return Ctx()
 
 
@@ -56,7 +57,7 @@ def test_a_layer_without_weights_is_refused(lib, monkeypatch):
     layer.ctx, layer.kv = h.ctx(), h.kv
     monkeypatch.setattr(B, "_stream", lambda: None)
     eviction = B.EvictionT(h.q, h.out, h.lse, 5, 0, 0)
-    eviction._keep = (None, None, torch.empty(2, 2, 5))
+    eviction._of = (2, 2)
     with pytest.raises(B.LosaError) as e:
         layer.evict(eviction)
     assert e.value.code == B.LOSA_ERR_INVALID_ARG
@@ -73,8 +74,8 @@ def test_tensors_of_another_shape_than_the_contexts_are_refused(lib, monkeypatch
         """Whether each of the three calls comes as far as the library, which refuses its null pointers."""
         q = torch.empty(shape, dtype=dtype)
         queries, eviction = B.QueriesT(None, 0, None, None, 3, 3, 0, 0, 1), B.EvictionT(None, None, None, 5, 0, 0)
-        queries._keep = (q, torch.empty(sequences + 1), None)
-        eviction._keep = (None, None, torch.empty(kept))
+        queries._keep, queries._of = (q, None, None), (*shape[1:], dtype, sequences)
+        eviction._of = kept[:2]
         lse = torch.empty(shape[:2])
         for call in (lambda: B.losa_window_attn(h.ctx(), queries, h.kv, q, lse), lambda: B.losa_kv_weights(h.ctx(), queries, h.kv, lse, weights),
                      lambda: B.losa_kv_evict(h.ctx(), h.kv, weights, eviction)):
